@@ -371,16 +371,16 @@ def _write(s, slots, positions):
     turned = torch.cat([a * cs - b * sn, b * cs + a * sn], -1).float().to(torch.bfloat16)
     live = (slots >= 0)
     s["q"].copy_(torch.where((positions >= 0)[:, None, None], turned[:, :H], s["q"]))
-    # (rows without a slot write what the last page's last row holds already, which no sequence uses)
+    # (rows without a slot write once more what the first row with one does; if there is none, what is there already)
     kc, ks, vc, vs = s["pool"]
-    slot = torch.where(live, slots, kc.shape[0] * ps - 1).long()
+    source = torch.where(live, torch.arange(T, device=DEV), live.int().argmax())
+    slot = slots[source].clamp(min=0).long()
     page, at = slot // ps, slot % ps
     for y, codes, scales in ((turned[:, H:], kc, ks), (x[:, H + G:].to(torch.bfloat16), vc, vs)):
         c, sc = _cast(y, kind, asym)
         c = c[..., 0::2] | c[..., 1::2] << 4
-        old_c, old_s = codes[page, :, at], scales[page, :, :, at]
-        codes[page, :, at] = torch.where(live[:, None, None], c, old_c)
-        scales[page, :, :, at] = torch.where(live.view(-1, *[1] * (sc.dim() - 1)), sc, old_s)
+        codes[page, :, at] = torch.where(live.any(), c[source], codes[page, :, at])
+        scales[page, :, :, at] = torch.where(live.any(), sc[source], scales[page, :, :, at])
 
 
 def _read(s, slots):
