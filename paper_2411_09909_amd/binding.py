@@ -1,5 +1,5 @@
-"""Thin ctypes binding of libamxfp4.so: the same entry points as include/amxfp4.h and include/amxfp4_layer.h, taking
-torch CUDA tensors. The calls of a serving loop, with all their buffers given, go through a small native module instead
+"""Thin ctypes binding of libamxfp4.so: the same entry points as include/amxfp4.h, include/amxfp4_layer.h and
+include/amxfp4_paged.h, taking torch CUDA tensors. The calls of a serving loop, with all their buffers given, go through a small native module instead
 (csrc/calls.cpp: a cast of one row 4.8 -> 3.3 us of host time); it leaves whatever it does not take to the code here.
 
 Only argument marshalling happens here (pointers, sizes, the current HIP stream); every step of the path runs in
@@ -10,6 +10,7 @@ import ctypes
 import os
 import threading
 import warnings
+from typing import NamedTuple
 
 import torch
 
@@ -27,6 +28,12 @@ class AmxFormat(ctypes.Structure):
 class AmxGemmOptions(ctypes.Structure):
     _fields_ = [("e5m2_kernel", ctypes.c_int32), ("pot_kernel", ctypes.c_int32), ("tile", ctypes.c_int32),
                 ("few_rows", ctypes.c_int32)]
+
+
+class AmxPagedPool(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("v_codes", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
 
 
 class AmxError(RuntimeError):
@@ -132,6 +139,17 @@ def _load():
                        ("amxfp4_rmsnorm_quantize", [fp, vp, vp, vp, vp, i64, i64, f32, vp, vp, vp])):
         getattr(L, name).argtypes = args
         getattr(L, name).restype = ctypes.c_int
+    pp = ctypes.POINTER(AmxPagedPool)
+    for name, args in (("amxfp4_paged_plan", [vp, vp] + [i64] * 5 + [vp] * 9),
+                       ("amxfp4_paged_write", [fp, pp, vp, i64, i64, i64, vp, vp, f64, vp, vp]),
+                       ("amxfp4_paged_read", [fp, pp, vp, i64, i32, vp, vp, vp]),
+                       ("amxfp4_paged_attention", [fp, pp, vp, i64, i64, vp, i64, i64, vp, vp, vp, f32, i64, vp, vp, ctypes.c_size_t, vp])):
+        getattr(L, name).argtypes = args
+        getattr(L, name).restype = ctypes.c_int
+    for name, args in (("amxfp4_paged_codes_bytes", [fp, pp]), ("amxfp4_paged_scales_bytes", [fp, pp]),
+                       ("amxfp4_paged_attention_workspace_bytes", [fp, pp, i64, i64, i64, i64])):
+        getattr(L, name).argtypes = args
+        getattr(L, name).restype = ctypes.c_size_t
     if calls is None:
         calls = _GeneralWay()
     else:
@@ -650,4 +668,164 @@ def merge_heads(o, groups, per_group, seq, head_dim):
     assert o.dtype == torch.float32 and o.is_contiguous()
     out = _bf16_out((seq, groups * per_group * head_dim), o.device)
     _check(load().amxfp4_merge_heads(o.data_ptr(), groups, per_group, seq, head_dim, out.data_ptr(), _stream()))
+    return out
+
+
+# ---- paged key / value cache (include/amxfp4_paged.h) ---------------------------------------------------------------
+
+class PagedPool(NamedTuple):
+    """The cache of one layer: codes u8 [pages, kv_heads, page_size, head_dim / 2], scales u8 [pages, kv_heads, head_dim / 32,
+    page_size(, 2)], of keys and of values."""
+    k_codes: torch.Tensor
+    k_scales: torch.Tensor
+    v_codes: torch.Tensor
+    v_scales: torch.Tensor
+
+
+class PagedPlan(NamedTuple):
+    """What paged_plan() writes, int32: lengths after the step [seqs], first rows [seqs + 1], slots and positions of the rows
+    [rows], {queue head, free pages, sequences refused, rows of all sequences} [4]."""
+    lens: torch.Tensor
+    starts: torch.Tensor
+    slots: torch.Tensor
+    positions: torch.Tensor
+    state: torch.Tensor
+
+
+def _here(*ts):
+    """All tensors on the current device, contiguous: what the calls of the paged cache take."""
+    _need_cuda(*ts)
+    at = torch._C._cuda_getDevice()
+    for t in ts:
+        if t.get_device() != at:
+            raise AmxError("a tensor on device %d, the current one is %d" % (t.get_device(), at))
+        if not t.is_contiguous():
+            raise AmxError("contiguous tensors only")
+
+
+def _ints(n, *ts):
+    for t in ts:
+        if t.dtype != torch.int32 or t.dim() != 1 or (n is not None and t.numel() != n):
+            raise AmxError("a one-dimensional int32 tensor%s needed, not %s of %s" % ("" if n is None else " of %d" % n, t.dtype, tuple(t.shape)))
+
+
+def _pool(fmt, pool):
+    """The C structure of a pool (four tensors as in PagedPool)."""
+    kc, ks, vc, vs = pool
+    _here(kc, ks, vc, vs)
+    if kc.dim() != 4 or any(t.dtype != torch.uint8 for t in pool):
+        raise AmxError("paged pool: four uint8 tensors, codes [pages, kv_heads, page_size, head_dim / 2]")
+    pages, heads, size, half = kc.shape
+    scales = (pages, heads, half // 16, size) + ((2,) if fmt.asymmetric else ())
+    if vc.shape != kc.shape or ks.shape != scales or vs.shape != scales:
+        raise AmxError("paged pool: scales of %s go with codes of %s in this format" % (scales, tuple(kc.shape)))
+    return AmxPagedPool(pages, size, heads, half * 2, 0, kc.data_ptr(), ks.data_ptr(), vc.data_ptr(), vs.data_ptr())
+
+
+def paged_pool(fmt, pages, kv_heads, head_dim, page_size, device="cuda"):
+    """An empty cache for one layer."""
+    codes = (pages, kv_heads, page_size, head_dim // 2)
+    scales = (pages, kv_heads, head_dim // 32, page_size) + ((2,) if fmt.asymmetric else ())
+    return PagedPool(*(torch.zeros(shape, dtype=torch.uint8, device=device) for shape in (codes, scales) * 2))
+
+
+def paged_plan(lens, new_rows, table, queue, state, page_size, rows=None, out=None):
+    """amxfp4_paged_plan: pages, slots and positions for one step. lens, new_rows int32 [seqs]; table int32 [seqs, max_pages] and
+    queue int32 [pages], updated in place; state int32 [4], left alone. rows: how many the packed batch has room for (default:
+    those of `out`, buffers as in PagedPlan). Returns a PagedPlan: its lens and state are the next step's."""
+    _here(lens, new_rows, table, queue, state)
+    seqs = lens.numel()
+    _ints(seqs, lens, new_rows)
+    _ints(None, queue)
+    _ints(4, state)
+    if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != seqs:
+        raise AmxError("paged_plan: table must be int32 [%d, max_pages]" % seqs)
+    if out is None:
+        if rows is None:
+            raise AmxError("paged_plan: rows or out needed")
+        out = [torch.empty(n, dtype=torch.int32, device=lens.device) for n in (seqs, seqs + 1, rows, rows, 4)]
+    plan = PagedPlan(*out)
+    rows = plan.slots.numel() if rows is None else rows
+    _here(*plan)
+    for n, t in zip((seqs, seqs + 1, rows, rows, 4), plan):
+        _ints(n, t)
+    _check(load().amxfp4_paged_plan(lens.data_ptr(), new_rows.data_ptr(), seqs, rows, page_size, queue.numel(), table.shape[1],
+                                    state.data_ptr(), queue.data_ptr(), table.data_ptr(), plan.lens.data_ptr(), plan.starts.data_ptr(),
+                                    plan.slots.data_ptr(), plan.positions.data_ptr(), plan.state.data_ptr(), _stream()))
+    return plan
+
+
+def paged_write(fmt, proj, pool, slots, positions, q_heads, theta, q=None):
+    """amxfp4_paged_write: proj FP32 [rows, ld] (queries | keys | values, rows contiguous) -> q BF16 [rows, q_heads, head_dim],
+    rotated; keys (rotated) and values cast into the pool at `slots`. Rows of negative position leave their q as it was (a new q is
+    zeroed)."""
+    p = _pool(fmt, pool)
+    _need_cuda(proj)
+    if proj.dtype != torch.float32 or proj.dim() != 2 or (proj.stride(1) != 1 and proj.shape[1] > 1):
+        raise AmxError("paged_write: proj must be float32 [rows, ld] with contiguous rows")
+    rows = proj.shape[0]
+    width = (q_heads + 2 * p.kv_heads) * p.head_dim
+    if proj.shape[1] < width:
+        raise AmxError("paged_write: proj has %d columns, %d query and 2 * %d other heads of %d need more" % (
+            proj.shape[1], q_heads, p.kv_heads, p.head_dim))
+    _here(slots, positions)
+    _ints(rows, slots, positions)
+    if q is None:
+        q = torch.zeros((rows, q_heads, p.head_dim), dtype=torch.bfloat16, device=proj.device)
+    _here(proj[:0], q)
+    if q.dtype != torch.bfloat16 or q.numel() != rows * q_heads * p.head_dim:
+        raise AmxError("paged_write: q must be bfloat16 [%d, %d, %d]" % (rows, q_heads, p.head_dim))
+    _check(load().amxfp4_paged_write(ctypes.byref(fmt), ctypes.byref(p), proj.data_ptr(), rows, proj.stride(0) if rows > 1 else width, q_heads,
+                                     slots.data_ptr(), positions.data_ptr(), theta, q.data_ptr(), _stream()))
+    return q
+
+
+def paged_read(fmt, pool, slots, k=None, v=None, dtype=torch.bfloat16):
+    """amxfp4_paged_read: keys and values at `slots`, dequantized: two tensors [rows, kv_heads, head_dim], BF16 or float32; zeros for
+    slots outside the pool."""
+    p = _pool(fmt, pool)
+    _here(slots)
+    _ints(None, slots)
+    shape = (slots.numel(), p.kv_heads, p.head_dim)
+    k = torch.empty(shape, dtype=dtype, device=slots.device) if k is None else k
+    v = torch.empty(shape, dtype=k.dtype, device=slots.device) if v is None else v
+    _here(k, v)
+    if tuple(k.shape) != shape or tuple(v.shape) != shape or k.dtype != v.dtype or k.dtype not in (torch.bfloat16, torch.float32):
+        raise AmxError("paged_read: k and v must be bfloat16 or float32 %s" % (shape,))
+    _check(load().amxfp4_paged_read(ctypes.byref(fmt), ctypes.byref(p), slots.data_ptr(), shape[0], 1 if k.dtype == torch.bfloat16 else 0,
+                                    k.data_ptr(), v.data_ptr(), _stream()))
+    return k, v
+
+
+def paged_attention_workspace_bytes(fmt, pool, rows, q_heads, seqs, max_keys):
+    p = _pool(fmt, pool)
+    return int(load().amxfp4_paged_attention_workspace_bytes(ctypes.byref(fmt), ctypes.byref(p), rows, q_heads, seqs, max_keys))
+
+
+def paged_attention(fmt, q, pool, table, lens, starts, positions, scale, max_keys=0, out=None, workspace=None):
+    """amxfp4_paged_attention: q BF16 [rows, q_heads, head_dim] against what the rows' sequences hold in the pool (lens, starts
+    and positions out of paged_plan()). max_keys: at least the longest sequence, 0 if not known. Returns BF16 [rows, q_heads *
+    head_dim]; rows behind the last sequence's are left as they were (zeros in a new tensor)."""
+    p = _pool(fmt, pool)
+    _here(q, table, lens, starts, positions)
+    if q.dtype != torch.bfloat16 or q.dim() != 3 or q.shape[2] != p.head_dim:
+        raise AmxError("paged_attention: q must be bfloat16 [rows, q_heads, %d]" % p.head_dim)
+    rows, q_heads, seqs = q.shape[0], q.shape[1], lens.numel()
+    _ints(seqs, lens)
+    _ints(seqs + 1, starts)
+    _ints(rows, positions)
+    if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != seqs:
+        raise AmxError("paged_attention: table must be int32 [%d, max_pages]" % seqs)
+    if out is None:
+        out = torch.zeros((rows, q_heads * p.head_dim), dtype=torch.bfloat16, device=q.device)
+    if out.dtype != torch.bfloat16 or out.numel() != q.numel():
+        raise AmxError("paged_attention: out must be bfloat16 [%d, %d]" % (rows, q_heads * p.head_dim))
+    if workspace is None:
+        need = int(load().amxfp4_paged_attention_workspace_bytes(ctypes.byref(fmt), ctypes.byref(p), rows, q_heads, seqs, max_keys))
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+    _here(out, workspace)
+    _check(load().amxfp4_paged_attention(ctypes.byref(fmt), ctypes.byref(p), q.data_ptr(), rows, q_heads, table.data_ptr(), seqs,
+                                         table.shape[1], lens.data_ptr(), starts.data_ptr(), positions.data_ptr(), float(scale),
+                                         int(max_keys), out.data_ptr(), workspace.data_ptr(),
+                                         workspace.numel() * workspace.element_size(), _stream()))
     return out
