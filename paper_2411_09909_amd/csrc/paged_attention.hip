@@ -1,4 +1,27 @@
-// Attention over the paged cache (include/amxfp4_paged.h).
+// Attention over the paged cache (include/amxfp4_paged.h): split over the keys, joined by a second kernel.
+//
+// Columns. A matrix instruction has 16 columns and a decoding step few rows of queries (4 query heads share a key head in the
+// models this is for), so the columns of a tile are (combination, group): a combination is a row and a query head that read
+// the same key head, a group one of the head dimension's D / 32 groups of the cast. Column (c, g) multiplies combination c with
+// group g of the keys alone (the query's other groups are zeros there), so that the group's scales, which are those of a token,
+// can be applied to the product: s[c][j] = sum_g S[j][g] (q . elements)[c][j][g]. The keys' elements are converted to BF16, which
+// holds them, and not scaled.
+//   sign pair   S_p q.e+ + S_n q.e- = (S_p + S_n) / 2 q.e + (S_p - S_n) / 2 q.|e|: two products, |e| by clearing sign bits. In FP32;
+//               what cancels is 2^-23 of the larger scale's share.
+//   (The codes as they are on the block-scaled instruction, the query as two E4M3 parts, saves the conversion and costs
+//   exactness: that instruction adds its products in a window of 2^-13 of the largest, and a score was off by 2^-12 of it.)
+// Values. The codes of 64 tokens are transposed by ds_read_b64_tr_b4 (16 lanes read 16 rows of 16 codes and get one column
+// each), converted to BF16 elements and multiplied with p[c][j] S[j][g], rounded to BF16: O[d][c] = sum_j (p S)[j][c] e[j][d].
+// The two sign classes stay apart here (e+ with p S_p, e- with p S_n): with (S_p + S_n) / 2 and (S_p - S_n) / 2 the rounding of the
+// larger class's weight would drown a smaller one. The columns of the other groups compute products nobody reads.
+// Layout of a tile of 64 tokens in a wave: lane (column or row r = l % 16, quarter u = l / 16). S^T comes out of the matrix
+// instruction t (of 4) with tile rows 4 u + i in lane (r, u): those rows are keys 16 u + 4 t + i, so that a lane holds the 16 keys
+// 16 u .. of its column, in the order in which the second product wants them, and needs the scales of 16 neighbouring tokens, 32 bytes.
+//
+// Division of the work: units of 64 tokens of one sequence, key head and tile of combinations, in that order, dealt out
+// evenly over the workgroups, whatever the sequences' lengths are. Every workgroup finds its own range from the lengths (a prefix sum
+// over the sequences, in LDS). A range may begin and end within a sequence: those partial results (O, m, l) go to the
+// workspace, at most two to a workgroup, and paged_attention_join_kernel adds them up.
 #include "paged.h"
 
 #include "kernels.h"
@@ -7,87 +30,575 @@
 namespace amx {
 namespace {
 
-// One workgroup to a row and query head, its four waves take turns with the keys, the lanes share out the head dimension; running
-// maximum and sum per wave, joined at the end.
-template <int SCALE_KIND, bool ASYM, int D>
-__global__ __launch_bounds__(256) void paged_attention_kernel(PagedPool pool, const uint16_t* __restrict__ q, int64_t rows, int q_heads,
-                                                              const int32_t* __restrict__ table, int seqs, int64_t max_pages,
-                                                              const int32_t* __restrict__ lens, const int32_t* __restrict__ starts,
-                                                              const int32_t* __restrict__ positions, float scale_log2,
-                                                              uint16_t* __restrict__ out) {
-  __shared__ float share[4][D + 2];
-  const int64_t t = blockIdx.x;
-  const int h = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int lo = 0, hi = seqs;  // the first sequence that ends behind the row
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (starts[mid + 1] > t)
-      hi = mid;
-    else
-      lo = mid + 1;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kTile = 64;        // tokens of a unit
+constexpr int kMostGroups = 1024;  // workgroups
+
+// What one launch reads.
+struct PagedWork {
+  const uint16_t* q;
+  const int32_t *table, *lens, *starts, *positions;
+  uint16_t* out;
+  uint8_t* workspace;
+  int64_t rows, max_pages;
+  int seqs, q_heads, per;  // per: query heads to a key head
+  float scale_log2;
+  int whole;  // a unit is a sequence, key head and tile of combinations with all its tokens
+};
+
+// What a workgroup leaves behind for the joining kernel, at the front of the workspace.
+struct PagedTail {
+  uint64_t units, end;    // all units; one past the last of the sequence, key head and tile that this workgroup began and did not end
+  uint32_t groups, owner;  // workgroups among which the units are divided; 1: it began such a one
+  int32_t seq, head, tile, pad;
+};
+
+// units of a workgroup: [first_unit(g), first_unit(g + 1))
+__device__ __forceinline__ uint64_t first_unit(uint64_t units, uint32_t groups, uint32_t g) {
+  return units / groups * g + (uint64_t)((units % groups) * g / groups);
+}
+
+template <int NC, int D>
+constexpr int kPartFloats = NC * (D + 2);
+
+__device__ __forceinline__ uint32_t divide(uint64_t a, uint64_t b, uint64_t& rest) {
+  if (((a | b) >> 32) == 0) {
+    const uint32_t q = (uint32_t)a / (uint32_t)b;
+    rest = (uint32_t)a - q * (uint32_t)b;
+    return q;
   }
-  if (lo >= seqs || starts[lo] > t) return;
-  const int64_t most = max_pages << pool.page_log2;
-  const int64_t keys = min(min((int64_t)positions[t] + 1, (int64_t)lens[lo]), most);
-  const int g = h / (q_heads / (int)pool.kv_heads);
-  constexpr int E = D / 64;  // elements of a lane
-  float qv[E], o[E] = {}, m = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) qv[e] = u2f((uint32_t)q[(t * q_heads + h) * D + lane * E + e] << 16);
-  for (int64_t j = wave; j < keys; j += 4) {
-    const uint32_t page = (uint32_t)table[lo * max_pages + (j >> pool.page_log2)];
-    if (page >= pool.pages) continue;
-    const int64_t page_head = (int64_t)page * pool.kv_heads + g, place = j & ((1 << pool.page_log2) - 1);
-    auto value = [&](const uint8_t* codes, const uint8_t* scales, int d) {
-      const uint32_t n = (codes[((page_head << pool.page_log2) + place) * (D / 2) + d / 2] >> (4 * (d & 1))) & 15u;
-      const int64_t s = ((page_head * (D / 32) + d / 32) << pool.page_log2) + place;
-      const float S = scale_value<SCALE_KIND>(ASYM ? scales[2 * s + (n >> 3)] : scales[s]);
-      return (float)e2m1_twice(n & 7u) * (n & 8u ? -0.5f * S : 0.5f * S);
-    };
-    float s = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) s += qv[e] * value(pool.k_codes, pool.k_scales, lane * E + e);
-#pragma unroll
-    for (int w = 32; w > 0; w >>= 1) s += __shfl_xor(s, w, 64);
-    s *= scale_log2;
-    const float m_new = fmaxf(m, s), alpha = __builtin_amdgcn_exp2f(m - m_new), p = __builtin_amdgcn_exp2f(s - m_new);
-    m = m_new, l = l * alpha + p;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = o[e] * alpha + p * value(pool.v_codes, pool.v_scales, lane * E + e);
+  const uint64_t q = a / b;
+  rest = a - q * b;
+  return (uint32_t)q;
+}
+
+// A sequence as the units see it. NT: tiles of tokens (one at least, so that a row without keys is written), CT: tiles of combinations.
+struct PagedSequence {
+  int64_t first;  // its first row
+  uint32_t rows, keys, NT, CT;
+};
+template <int NC>
+__device__ __forceinline__ PagedSequence paged_sequence(const PagedWork& w, const PagedPool& pool, int b) {
+  PagedSequence s;
+  const int64_t a = max((int64_t)w.starts[b], (int64_t)0), e = min((int64_t)w.starts[b + 1], w.rows);
+  const int64_t n = w.lens[b];
+  s.first = a;
+  s.rows = e > a ? (uint32_t)(e - a) : 0u;
+  s.keys = (uint32_t)max((int64_t)0, min(n, w.max_pages << pool.page_log2));
+  s.NT = max((s.keys + kTile - 1) / kTile, 1u);
+  s.CT = (uint32_t)(((uint64_t)s.rows * w.per + NC - 1) / NC);
+  return s;
+}
+
+// max over the four quarters of a wave (lanes of the same column)
+__device__ __forceinline__ float quarters_max(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(f2u(v), f2u(v), false, false);
+  v = fmaxf(u2f(a[0]), u2f(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(f2u(v), f2u(v), false, false);
+  return fmaxf(u2f(b[0]), u2f(b[1]));
+}
+__device__ __forceinline__ float quarters_sum(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(f2u(v), f2u(v), false, false);
+  v = u2f(a[0]) + u2f(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(f2u(v), f2u(v), false, false);
+  return u2f(b[0]) + u2f(b[1]);
+}
+
+// sum over the GC neighbouring columns of a combination (1, 2 or 4 lanes)
+template <int GC>
+__device__ __forceinline__ float columns_sum(float v) {
+  if constexpr (GC >= 2) v += u2f((uint32_t)__builtin_amdgcn_mov_dpp((int)f2u(v), 0xB1, 0xF, 0xF, true));
+  if constexpr (GC >= 4) v += u2f((uint32_t)__builtin_amdgcn_mov_dpp((int)f2u(v), 0x4E, 0xF, 0xF, true));
+  return v;
+}
+
+// Two scales (bytes 2 HALF and 2 HALF + 1 of a word) as floats.
+template <int SCALE_KIND, bool HALF>
+__device__ __forceinline__ f32x2 two_scales(uint32_t word) {
+  if constexpr (SCALE_KIND == kScaleE5M2) {
+    return __builtin_amdgcn_cvt_pk_f32_bf8((int)word, HALF);
+  } else if constexpr (SCALE_KIND == kScaleE4M3) {
+    return __builtin_amdgcn_cvt_pk_f32_fp8((int)word, HALF);
+  } else {  // the exponent's field (byte 0: 2^-127, as good as the 0 it becomes)
+    const uint32_t a = HALF ? word << 7 : word << 23, b = HALF ? word >> 1 : word << 15;
+    return f32x2{u2f(a & 0x7F800000u), u2f(b & 0x7F800000u)};
   }
-#pragma unroll
-  for (int e = 0; e < E; ++e) share[wave][lane * E + e] = o[e];
-  share[wave][D] = m, share[wave][D + 1] = l;
-  __syncthreads();
-  if (threadIdx.x < D) {
-    const float top = fmaxf(fmaxf(share[0][D], share[1][D]), fmaxf(share[2][D], share[3][D]));
-    float sum = 0.f, total = 0.f;
-    for (int w = 0; w < 4; ++w) {
-      const float f = share[w][D] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(share[w][D] - top);
-      sum += share[w][threadIdx.x] * f, total += share[w][D + 1] * f;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
+}
+
+// eight codes -> eight elements, BF16
+__device__ __forceinline__ u32x4 elements(uint32_t word) {
+  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, 1.0f, 0)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, 1.0f, 1)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, 1.0f, 2)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, 1.0f, 3))};
+}
+
+template <int SCALE_KIND, bool ASYM, int D, int GC>
+struct PagedTile {
+  static constexpr int kGroups = D / 32, GS = kGroups / GC;
+  static constexpr int NK = D / 32, NV = D / 32;          // loads of 16 bytes: codes of K, of V
+  static constexpr int kScaleWords = (ASYM ? 8 : 4);      // scales of 16 tokens
+  u32x4 k[NK], v[NV];
+  u32x4 ks[GS][kScaleWords / 4], vs[GS][kScaleWords / 4];
+  uint32_t bad;  // sub-blocks of 16 tokens whose page is none
+};
+
+template <int SCALE_KIND, bool ASYM, int D, int GC>
+__global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void paged_attention_kernel(PagedPool pool, PagedWork w) {
+  using Tile = PagedTile<SCALE_KIND, ASYM, D, GC>;
+  constexpr int GS = Tile::GS, NC = 16 / GC, DT = D / 16;
+  constexpr int kValueBytes = kTile * D / 2;  // of a wave's tile of V
+  constexpr int kShareFloats = NC * D;
+  extern __shared__ __align__(16) uint8_t lds[];
+  uint64_t* ends = reinterpret_cast<uint64_t*>(lds);  // units up to and with a sequence
+  uint8_t* region = lds + (((size_t)w.seqs * 8 + 15) & ~(size_t)15);
+  __shared__ uint64_t edge[4];
+  __shared__ float top_of[4][NC], sum_of[4][NC];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, u = lane >> 4, c = r / GC, gc = r % GC;
+  uint8_t* const mine = region + wave * kValueBytes;
+
+  // ---- the workgroup's range of units
+  {
+    const int each = (w.seqs + 255) >> 8, b0 = threadIdx.x * each, b1 = min(w.seqs, b0 + each);
+    uint64_t sum = 0;
+    for (int b = b0; b < b1; ++b) {
+      const PagedSequence s = paged_sequence<NC>(w, pool, b);
+      sum += (uint64_t)pool.kv_heads * s.CT * (w.whole ? 1 : s.NT);
+      ends[b] = sum;
     }
-    out[(t * q_heads + h) * D + threadIdx.x] = (uint16_t)bf16_rne(total > 0.f ? sum / total : 0.f);
+    uint64_t upto = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint64_t v = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += v;
+    }
+    if (lane == 63) edge[wave] = upto;
+    __syncthreads();
+    uint64_t before = upto - sum;
+    for (int i = 0; i < wave; ++i) before += edge[i];
+    for (int b = b0; b < b1; ++b) ends[b] += before;
+    __syncthreads();
   }
+  const uint64_t units = ends[w.seqs - 1];
+  const uint64_t busy = w.whole ? units : (units + 3) / 4;  // a tile to each wave at least
+  const uint32_t groups = (uint32_t)max((uint64_t)1, min((uint64_t)gridDim.x, busy)), g = blockIdx.x;
+  PagedTail* tail = reinterpret_cast<PagedTail*>(w.workspace) + g;
+  if (threadIdx.x == 0 && !w.whole) *tail = PagedTail{units, 0, groups, 0, 0, 0, 0, 0};
+  if (g >= groups || units == 0) return;
+  const uint64_t lo = first_unit(units, groups, g), hi = first_unit(units, groups, g + 1);
+  int b = 0;
+  for (int step = w.seqs; step > 0;) {  // the first sequence whose units end behind lo
+    const int half = step >> 1, mid = b + half;
+    if (ends[mid] <= lo)
+      b = mid + 1, step -= half + 1;
+    else
+      step = half;
+  }
+
+  for (uint64_t unit = lo; unit < hi;) {
+    while (ends[b] <= unit) ++b;
+    const PagedSequence s = paged_sequence<NC>(w, pool, b);
+    const uint64_t base = b ? ends[b - 1] : 0;
+    uint64_t tile64, ct64;
+    const uint32_t NT = w.whole ? 1 : s.NT;
+    const uint32_t seg = divide(unit - base, NT, tile64);
+    const uint32_t head = divide(seg, s.CT, ct64), ct = (uint32_t)ct64;
+    const uint32_t t0 = (uint32_t)tile64;
+    const uint64_t after = base + ((uint64_t)seg + 1) * NT;  // the unit behind this segment's last
+    const uint32_t t1 = w.whole ? s.NT : (uint32_t)min((uint64_t)NT, t0 + (hi - unit));
+    const int32_t* row_table = w.table + (int64_t)b * w.max_pages;
+    const uint32_t last_entry = (uint32_t)(w.max_pages - 1);
+
+    // ---- this lane's combination
+    const uint64_t combination = (uint64_t)ct * NC + c;
+    const bool asked = combination < (uint64_t)s.rows * w.per;
+    const uint32_t row_of = asked ? (uint32_t)(combination / (uint32_t)w.per) : 0u, head_of = asked ? (uint32_t)(combination % (uint32_t)w.per) : 0u;
+    const int64_t row = s.first + row_of;
+    // tokens it sees; columns that nobody asked for see all and are not looked at
+    const int limit = asked ? min(max(w.positions[row], -1) + 1, (int)s.keys) : 0x7FFFFFFF;
+    int least = limit, most = asked ? limit : 0;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) least = min(least, __shfl_xor(least, o, 64)), most = max(most, __shfl_xor(most, o, 64));
+    least = __builtin_amdgcn_readfirstlane(least), most = __builtin_amdgcn_readfirstlane(most);
+    const uint32_t stop = min(t1, (uint32_t)(most + kTile - 1) / kTile);
+
+    // ---- requests
+    const int64_t page_stride = (int64_t)pool.kv_heads << pool.page_log2;
+    auto request = [&](uint32_t tile, Tile& d) {
+      uint32_t id[4];
+      d.bad = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t entry = min((tile * kTile + 16 * k) >> pool.page_log2, last_entry);
+        id[k] = (uint32_t)__builtin_amdgcn_readfirstlane(row_table[entry]);
+        if (id[k] >= pool.pages) d.bad |= 1u << k, id[k] = 0;
+      }
+      const uint32_t mask = (1u << pool.page_log2) - 1;
+      auto pick = [&](int k) {  // the id of a sub-block that depends on the lane
+        const uint32_t a = k & 1 ? id[1] : id[0], z = k & 1 ? id[3] : id[2];
+        return k & 2 ? z : a;
+      };
+      auto first_token = [&](uint32_t page, uint32_t token) {  // of the pool, for this head: place of a token
+        return (int64_t)page * page_stride + ((int64_t)head << pool.page_log2) + (token & mask);
+      };
+      // K: tile row r of product t is key 16 (r / 4) + 4 t + r % 4
+      {
+        const int k = r >> 2;
+        const uint32_t token = tile * kTile + 16 * k + (r & 3) + (D == 64 ? 4 * (u >> 1) : 0);
+        const uint8_t* p = pool.k_codes + first_token(pick(k), token) * (D / 2) + 16 * (D == 64 ? (u & 1) : u);
+#pragma unroll
+        for (int t = 0; t < Tile::NK; ++t) d.k[t] = *reinterpret_cast<const u32x4*>(p + t * (D == 64 ? 8 : 4) * (D / 2));
+      }
+#pragma unroll
+      for (int n = 0; n < Tile::NV; ++n) {
+        constexpr int kParts = D / 32;  // pieces of 16 bytes in a row
+        const uint32_t at = n * (64 / kParts) + lane / kParts, token = tile * kTile + at;
+        const uint32_t page = D == 128 ? id[n] : (lane < 32 ? id[2 * n & 3] : id[(2 * n + 1) & 3]);
+        d.v[n] = *reinterpret_cast<const u32x4*>(pool.v_codes + first_token(page, token) * (D / 2) + 16 * (lane % kParts));
+      }
+      // scales of tokens 16 u .. of group s * GC + gc
+      {
+        const uint32_t token = (tile * kTile + 16 * u) & mask;
+        const int64_t at = (((int64_t)pick(u) * pool.kv_heads + head) * Tile::kGroups + gc) << pool.page_log2;
+        const int64_t offset = (at + token) * (ASYM ? 2 : 1);
+#pragma unroll
+        for (int st = 0; st < GS; ++st)
+#pragma unroll
+          for (int i = 0; i < Tile::kScaleWords / 4; ++i) {
+            const int64_t o = offset + (((int64_t)st * GC) << pool.page_log2) * (ASYM ? 2 : 1) + 16 * i;
+            d.ks[st][i] = *reinterpret_cast<const u32x4*>(pool.k_scales + o);
+            d.vs[st][i] = *reinterpret_cast<const u32x4*>(pool.v_scales + o);
+          }
+      }
+    };
+    Tile next;
+    uint32_t tile = t0 + wave;
+    if (tile < stop) request(tile, next);
+
+    // ---- the query: dimensions 32 j + 8 u .. of group j, zeros where the column is not the group's
+    u32x4 q[Tile::kGroups];
+#pragma unroll
+    for (int j = 0; j < Tile::kGroups; ++j) {
+      q[j] = u32x4{0, 0, 0, 0};
+      if (asked && j % GC == gc)
+        q[j] = *reinterpret_cast<const u32x4*>(w.q + (row * w.q_heads + (int64_t)head * w.per + head_of) * D + 32 * j + 8 * u);
+    }
+
+    // ---- the tiles
+    f32x4 o[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i) o[i] = f32x4{0, 0, 0, 0};
+    float m = -INFINITY, l = 0.f;
+    const float sc = ASYM ? 0.5f * w.scale_log2 : w.scale_log2;
+
+    for (; tile < stop; tile += 4) {
+      const Tile d = next;
+      // V into LDS, piece p of row j at p ^ (some bits of j): rows that 16 lanes read at once lie in different banks
+#pragma unroll
+      for (int n = 0; n < Tile::NV; ++n) {
+        constexpr int kParts = D / 32;
+        const int j = n * (64 / kParts) + lane / kParts, part = (lane % kParts) ^ (D == 128 ? (j >> 2) & 3 : (j >> 3) & 1);
+        *reinterpret_cast<u32x4*>(mine + j * (D / 2) + 16 * part) = d.v[n];
+      }
+      if (tile + 4 < stop) request(tile + 4, next);
+
+      // ---- scores
+      float x[16];
+      const int first = (int)tile * kTile;
+      const int count = (d.bad >> u) & 1 ? 0 : max(0, min(limit - first - 16 * u, 16));
+      const bool all = first + kTile <= least && d.bad == 0;
+      uint32_t kw[4 * Tile::NK];
+#pragma unroll
+      for (int n = 0; n < Tile::NK; ++n) {
+        // a lane has the four words of one group; it is to have word u of each of the four: the quarters' 4 x 4 words transposed
+        const auto a = __builtin_amdgcn_permlane32_swap(d.k[n][0], d.k[n][2], false, false);
+        const auto z = __builtin_amdgcn_permlane32_swap(d.k[n][1], d.k[n][3], false, false);
+        const auto y0 = __builtin_amdgcn_permlane16_swap(a[0], z[0], false, false), y1 = __builtin_amdgcn_permlane16_swap(a[1], z[1], false, false);
+        kw[4 * n] = y0[0], kw[4 * n + 1] = y0[1], kw[4 * n + 2] = y1[0], kw[4 * n + 3] = y1[1];
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[4 * t + i] = 0.f;
+#pragma unroll
+        for (int st = 0; st < GS; ++st) {
+          f32x4 dot = {0, 0, 0, 0}, with = {0, 0, 0, 0};
+#pragma unroll
+          for (int j = st * GC; j < (st + 1) * GC; ++j) {
+            const u32x4 e = elements(kw[Tile::kGroups * t + j]);  // (heads of 64: two tiles' words in turn)
+            const bf16x8 qj = __builtin_bit_cast(bf16x8, q[j]);
+            dot = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, e), qj, dot, 0, 0, 0);
+            if constexpr (ASYM) with = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, e & 0x7FFF7FFFu), qj, with, 0, 0, 0);
+          }
+          if constexpr (ASYM) {
+            const uint32_t s0 = d.ks[st][t >> 1][2 * t & 3], s1 = d.ks[st][t >> 1][(2 * t + 1) & 3];
+            const f32x2 a[4] = {two_scales<SCALE_KIND, false>(s0), two_scales<SCALE_KIND, true>(s0), two_scales<SCALE_KIND, false>(s1),
+                                two_scales<SCALE_KIND, true>(s1)};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              x[4 * t + i] += __builtin_fmaf(a[i][0] + a[i][1], dot[i], (a[i][0] - a[i][1]) * with[i]);
+          } else {
+            const uint32_t s0 = d.ks[st][0][t];
+            const f32x2 a = two_scales<SCALE_KIND, false>(s0), z = two_scales<SCALE_KIND, true>(s0);
+            x[4 * t] = __builtin_fmaf(a[0], dot[0], x[4 * t]), x[4 * t + 1] = __builtin_fmaf(a[1], dot[1], x[4 * t + 1]);
+            x[4 * t + 2] = __builtin_fmaf(z[0], dot[2], x[4 * t + 2]), x[4 * t + 3] = __builtin_fmaf(z[1], dot[3], x[4 * t + 3]);
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = columns_sum<GC>(x[i]);
+      if (!all) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = i < count ? x[i] : -INFINITY;
+      }
+
+      // ---- running maximum and sum
+      float top = x[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+      top = fmaxf(m, quarters_max(top));
+      const float to = top == -INFINITY ? 0.f : top, alpha = __builtin_amdgcn_exp2f((m - to) * sc), shift = to * sc;
+      m = top;
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], sc, -shift)), sum += x[i];
+      l = __builtin_fmaf(l, alpha, sum);
+      if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[i] *= alpha;
+      }
+
+      // ---- values
+#pragma unroll
+      for (int st = 0; st < GS; ++st) {
+        uint32_t wp[8], wn[8];  // weights of this lane's 16 keys, pairs
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          f32x2 s0, s1;  // (S_p, S_n) of keys 2 i and 2 i + 1
+          if constexpr (ASYM) {
+            const uint32_t word = d.vs[st][i >> 2][i & 3];
+            s0 = two_scales<SCALE_KIND, false>(word), s1 = two_scales<SCALE_KIND, true>(word);
+          } else {
+            const uint32_t word = d.vs[st][0][i >> 1];
+            const f32x2 pair = i & 1 ? two_scales<SCALE_KIND, true>(word) : two_scales<SCALE_KIND, false>(word);
+            s0 = f32x2{pair[0], pair[0]}, s1 = f32x2{pair[1], pair[1]};
+          }
+          if (!all) {  // (what lies behind the last token may be infinite)
+            if (2 * i >= count) s0 = f32x2{0, 0};
+            if (2 * i + 1 >= count) s1 = f32x2{0, 0};
+          }
+          wp[i] = pack_bf16(x[2 * i] * s0[0], x[2 * i + 1] * s1[0]);
+          if constexpr (ASYM) wn[i] = pack_bf16(x[2 * i] * s0[1], x[2 * i + 1] * s1[1]);
+        }
+        const bf16x8 p0 = __builtin_bit_cast(bf16x8, (u32x4{wp[0], wp[1], wp[2], wp[3]})), p1 = __builtin_bit_cast(bf16x8, (u32x4{wp[4], wp[5], wp[6], wp[7]}));
+        bf16x8 n0, n1;
+        if constexpr (ASYM)
+          n0 = __builtin_bit_cast(bf16x8, (u32x4{wn[0], wn[1], wn[2], wn[3]})), n1 = __builtin_bit_cast(bf16x8, (u32x4{wn[4], wn[5], wn[6], wn[7]}));
+#pragma unroll
+        for (int dt = 2 * GC * st; dt < 2 * GC * (st + 1); ++dt) {
+          const int j = 16 * u + r, part = (dt >> 1) ^ (D == 128 ? (j >> 2) & 3 : (j >> 3) & 1);
+          typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+          const i32x2 codes = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2*)(mine + j * (D / 2) + 16 * part + 8 * (dt & 1)));
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const u32x4 e = elements((uint32_t)codes[h]);
+            if constexpr (ASYM) {
+              uint32_t pos[4], neg[4];  // as 16-bit integers negative numbers lie below 0
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const uint32_t two = e[i];  // (a bit cast of the vector's element itself takes element 0)
+                const i16x2 v = __builtin_bit_cast(i16x2, two), z = {0, 0};
+                pos[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(v, z));
+                neg[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(v, z));
+              }
+              o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, (u32x4{pos[0], pos[1], pos[2], pos[3]})), h ? p1 : p0, o[dt], 0, 0, 0);
+              o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, (u32x4{neg[0], neg[1], neg[2], neg[3]})), h ? n1 : n0, o[dt], 0, 0, 0);
+            } else {
+              o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, e), h ? p1 : p0, o[dt], 0, 0, 0);
+            }
+          }
+        }
+      }
+    }
+
+    // ---- the four waves' shares, each against its own maximum, become one
+    l = quarters_sum(l);
+    if (u == 0 && gc == 0) top_of[wave][c] = m, sum_of[wave][c] = l;
+    __syncthreads();  // (and all waves have read their V)
+    const float top = fmaxf(fmaxf(top_of[0][c], top_of[1][c]), fmaxf(top_of[2][c], top_of[3][c]));
+    const float factor = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * sc);
+    float* share = reinterpret_cast<float*>(region);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+      if ((dt >> 1) % GC == gc) *reinterpret_cast<f32x4*>(share + wave * kShareFloats + c * D + dt * 16 + 4 * u) = o[dt] * factor;
+    __syncthreads();
+    const bool complete = w.whole || (t0 == 0 && t1 == NT);
+    float* part = nullptr;
+    if (!complete)  // slot 0: begun by another workgroup, 1: begun here
+      part = reinterpret_cast<float*>(w.workspace + (((size_t)gridDim.x * sizeof(PagedTail) + 255) & ~(size_t)255)) +
+             (2 * (size_t)g + (t0 == 0 ? 1 : 0)) * kPartFloats<NC, D>;
+    for (int i = threadIdx.x; i < kShareFloats / 2; i += 256) {
+      const int combo = 2 * i / D, dim = 2 * i % D;
+      float2 v = *reinterpret_cast<const float2*>(share + 2 * i);
+#pragma unroll
+      for (int k = 1; k < 4; ++k) {
+        const float2 z = *reinterpret_cast<const float2*>(share + k * kShareFloats + 2 * i);
+        v.x += z.x, v.y += z.y;
+      }
+      float best = top_of[0][combo], total = 0.f;
+#pragma unroll
+      for (int k = 1; k < 4; ++k) best = fmaxf(best, top_of[k][combo]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) total += top_of[k][combo] == -INFINITY ? 0.f : sum_of[k][combo] * __builtin_amdgcn_exp2f((top_of[k][combo] - best) * sc);
+      if (complete) {
+        const uint64_t which = (uint64_t)ct * NC + combo;
+        if (which < (uint64_t)s.rows * w.per) {
+          const float inv = total > 0.f ? 1.0f / total : 0.f;
+          const int64_t to = ((s.first + (int64_t)(which / (uint32_t)w.per)) * w.q_heads + (int64_t)head * w.per + (int64_t)(which % (uint32_t)w.per)) * D + dim;
+          *reinterpret_cast<uint32_t*>(w.out + to) = pack_bf16(v.x * inv, v.y * inv);
+        }
+      } else {
+        *reinterpret_cast<float2*>(part + 2 * i) = v;
+        if (dim == 0) part[NC * D + combo] = best * sc, part[NC * D + NC + combo] = total;
+      }
+    }
+    if (!complete && t0 == 0 && threadIdx.x == 0) *tail = PagedTail{units, after, groups, 1, b, (int32_t)head, (int32_t)ct, 0};
+    __syncthreads();  // the share has been read
+    unit += w.whole ? 1 : t1 - t0;
+  }
+}
+
+// Adds up the partial results of one sequence, key head and tile of combinations: the second slot of the workgroup that began it,
+// then the first slots of those after it, in their order. One workgroup to a workgroup of the other kernel and a combination; most
+// have nothing to do.
+template <int D, int NC>
+__global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedPool pool, PagedWork w, uint32_t grid) {
+  constexpr int kLanes = D / 4, kParts = 256 / kLanes;
+  const uint32_t g = blockIdx.x;
+  const int combo = blockIdx.y;
+  const PagedTail t = reinterpret_cast<const PagedTail*>(w.workspace)[g];
+  if (!t.owner) return;
+  const PagedSequence s = paged_sequence<NC>(w, pool, t.seq);
+  const uint64_t which = (uint64_t)(uint32_t)t.tile * NC + combo;
+  if (which >= (uint64_t)s.rows * w.per) return;
+  // the workgroup that has the segment's last unit: about (end - 1) groups / units
+  uint32_t last = (uint32_t)((double)(t.end - 1) * t.groups / (double)t.units);
+  last = min(last, t.groups - 1);
+  while (last + 1 < t.groups && first_unit(t.units, t.groups, last + 1) < t.end) ++last;
+  while (first_unit(t.units, t.groups, last) >= t.end) --last;
+  const uint32_t count = last - g + 1;
+  const float* parts = reinterpret_cast<const float*>(w.workspace + (((size_t)grid * sizeof(PagedTail) + 255) & ~(size_t)255));
+  auto part = [&](uint32_t i) { return parts + (2 * (size_t)(g + i) + (i == 0 ? 1 : 0)) * kPartFloats<NC, D>; };
+  __shared__ float tops[kMostGroups], red[4];
+  __shared__ float4 sums[kParts][kLanes];
+  __shared__ float totals[kParts];
+  float top = -INFINITY;
+  for (uint32_t i = threadIdx.x; i < count; i += 256) {
+    const float v = part(i)[NC * D + combo];
+    tops[i] = v;
+    top = fmaxf(top, v);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  const int mine = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+  float4 sum = make_float4(0, 0, 0, 0);
+  float total = 0.f;
+  for (uint32_t i = mine; i < count; i += kParts) {
+    const float f = tops[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(tops[i] - top);
+    const float* p = part(i);
+    const float4 v = *reinterpret_cast<const float4*>(p + combo * D + 4 * lane);
+    sum.x += v.x * f, sum.y += v.y * f, sum.z += v.z * f, sum.w += v.w * f;
+    total += p[NC * D + NC + combo] * f;
+  }
+  sums[mine][lane] = sum;
+  if (lane == 0) totals[mine] = total;
+  __syncthreads();
+  if (mine != 0) return;
+#pragma unroll
+  for (int k = 1; k < kParts; ++k) {
+    const float4 v = sums[k][lane];
+    sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+    total += totals[k];
+  }
+  const float inv = total > 0.f ? 1.0f / total : 0.f;
+  const int64_t to = ((s.first + (int64_t)(which / (uint32_t)w.per)) * w.q_heads + (int64_t)t.head * w.per + (int64_t)(which % (uint32_t)w.per)) * D + 4 * lane;
+  *reinterpret_cast<uint2*>(w.out + to) = make_uint2(pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv));
+}
+
+// Columns to a combination: as many of the groups as leave room for the combinations that a sequence has on average. (Shares of
+// 16 combinations and the sums of more than 2048 sequences would not fit the 64 KB of LDS of a launch.)
+int columns_of(int head_dim, int64_t rows, int64_t seqs, int64_t per) {
+  const int64_t combinations = per * ((rows + seqs - 1) / seqs);
+  if (head_dim == 128 && combinations <= 4) return 4;
+  return combinations <= 8 || seqs > 2048 ? 2 : 1;
+}
+
+// Tokens up to which a sequence is not split over workgroups.
+bool is_whole(int64_t most_keys) { return most_keys <= 512; }
+
+// Workgroups: no more than there can be units.
+int64_t groups_of(int nc, int64_t rows, int64_t seqs, int64_t per, int64_t kv_heads, int64_t most_keys) {
+  const int64_t tiles = rows * per / nc + (seqs < rows ? seqs : rows);  // at most: of combinations, of all sequences
+  const int64_t units = is_whole(most_keys) ? 1 : ((most_keys + kTile - 1) / kTile + 3) / 4;
+  return tiles >= kMostGroups || tiles * kv_heads >= kMostGroups || units >= kMostGroups || tiles * kv_heads * units >= kMostGroups
+             ? kMostGroups
+             : tiles * kv_heads * units;
 }
 
 }  // namespace
 
-size_t paged_attention_workspace(int, int64_t, int64_t, int64_t, int64_t, int64_t) { return 0; }
+size_t paged_attention_workspace(int head_dim, int64_t rows, int64_t q_heads, int64_t kv_heads, int64_t seqs, int64_t) {
+  // (whatever max_keys says: a sequence may be longer)
+  const int64_t nc = 16 / columns_of(head_dim, rows, seqs, q_heads / kv_heads);
+  return ((kMostGroups * sizeof(PagedTail) + 255) & ~(size_t)255) + 2 * kMostGroups * nc * (head_dim + 2) * sizeof(float);
+}
 
 hipError_t launch_paged_attention(int scale_kind, bool asym, int head_dim, const PagedPool& pool, const uint16_t* q, int64_t rows,
                                   int64_t q_heads, const int32_t* table, int64_t seqs, int64_t max_pages, const int32_t* lens,
                                   const int32_t* starts, const int32_t* positions, float scale, int64_t max_keys, uint16_t* out,
                                   void* workspace, hipStream_t s) {
-  auto go = [&]<int SK, bool ASYM>() {
-    auto kernel = head_dim == 128 ? paged_attention_kernel<SK, ASYM, 128> : paged_attention_kernel<SK, ASYM, 64>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)rows, (unsigned)q_heads), dim3(256), 0, s, pool, q, rows, (int)q_heads, table, (int)seqs,
-                       max_pages, lens, starts, positions, scale * 1.4426950408889634f, out);
+  const int64_t per = q_heads / pool.kv_heads, width = max_pages << pool.page_log2;
+  const int64_t most_keys = max_keys > 0 && max_keys < width ? max_keys : width;
+  const int gc = columns_of(head_dim, rows, seqs, per), nc = 16 / gc;
+  const bool whole = is_whole(most_keys);
+  const int64_t grid = groups_of(nc, rows, seqs, per, pool.kv_heads, most_keys);
+  const PagedWork w = {q, table, lens, starts, positions, out, static_cast<uint8_t*>(workspace), rows, max_pages, (int)seqs, (int)q_heads,
+                       (int)per, scale * 1.4426950408889634f, whole ? 1 : 0};
+  const size_t values = 4 * kTile * (size_t)head_dim / 2, shares = 4 * (size_t)nc * head_dim * sizeof(float);
+  const size_t lds = (((size_t)seqs * 8 + 15) & ~(size_t)15) + (values > shares ? values : shares);
+  auto go = [&]<int SK, bool ASYM, int D, int GC>() {
+    hipLaunchKernelGGL((paged_attention_kernel<SK, ASYM, D, GC>), dim3((unsigned)grid), dim3(256), lds, s, pool, w);
+    if (!whole)
+      hipLaunchKernelGGL((paged_attention_join_kernel<D, 16 / GC>), dim3((unsigned)grid, 16 / GC), dim3(256), 0, s, pool, w, (uint32_t)grid);
     return hipGetLastError();
   };
+  auto with_format = [&]<int SK, bool ASYM>() {
+    if (head_dim == 128)
+      return gc == 4 ? go.template operator()<SK, ASYM, 128, 4>()
+             : gc == 2 ? go.template operator()<SK, ASYM, 128, 2>()
+                       : go.template operator()<SK, ASYM, 128, 1>();
+    return gc == 2 ? go.template operator()<SK, ASYM, 64, 2>() : go.template operator()<SK, ASYM, 64, 1>();
+  };
   switch (scale_kind) {
-    case kScaleE5M2: return asym ? go.template operator()<kScaleE5M2, true>() : go.template operator()<kScaleE5M2, false>();
-    case kScaleE4M3: return asym ? go.template operator()<kScaleE4M3, true>() : go.template operator()<kScaleE4M3, false>();
-    default: return asym ? go.template operator()<kScaleE8M0Floor, true>() : go.template operator()<kScaleE8M0Floor, false>();
+    case kScaleE5M2: return asym ? with_format.template operator()<kScaleE5M2, true>() : with_format.template operator()<kScaleE5M2, false>();
+    case kScaleE4M3: return asym ? with_format.template operator()<kScaleE4M3, true>() : with_format.template operator()<kScaleE4M3, false>();
+    default: return asym ? with_format.template operator()<kScaleE8M0Floor, true>() : with_format.template operator()<kScaleE8M0Floor, false>();
   }
 }
 

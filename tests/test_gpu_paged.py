@@ -429,7 +429,7 @@ def test_conversations_step_by_step(captured):
                 want, tol = dense(history[b], n, H, G, D, s.scale, kind, asym)
                 worst = np.abs(mine - want) - tol
                 at = np.unravel_index(worst.argmax(), worst.shape)
-                assert (worst <= 0).all(), (new, b, len(history[b]), at, mine[at], want[at], tol[at], (worst > 0).sum())
+                assert (worst <= 0).all(), (new, b, len(history[b]), [float(v) for v in (*at, mine[at], want[at], tol[at])], int((worst > 0).sum()))
             assert lens[b] == len(history[b])
         assert (got[starts[-1]:] == 7.0).all()
         torch.randn(1000, device="cuda").sum().item()   # eager work between the replays
