@@ -733,6 +733,10 @@ def paged_plan(lens, new_rows, table, queue, state, page_size, rows=None, out=No
     """amxfp4_paged_plan: pages, slots and positions for one step. lens, new_rows int32 [seqs]; table int32 [seqs, max_pages] and
     queue int32 [pages], updated in place; state int32 [4], left alone. rows: how many the packed batch has room for (default:
     those of `out`, buffers as in PagedPlan). Returns a PagedPlan: its lens and state are the next step's."""
+    if out is not None and rows is None:
+        rc = (_calls or _bound()).paged_plan(lens, new_rows, table, queue, state, page_size, out)
+        if rc is not None:
+            return _check(rc) if rc else out if type(out) is PagedPlan else PagedPlan(*out)
     _here(lens, new_rows, table, queue, state)
     seqs = lens.numel()
     _ints(seqs, lens, new_rows)
@@ -759,6 +763,10 @@ def paged_write(fmt, proj, pool, slots, positions, q_heads, theta, q=None):
     """amxfp4_paged_write: proj FP32 [rows, ld] (queries | keys | values, rows contiguous) -> q BF16 [rows, q_heads, head_dim],
     rotated; keys (rotated) and values cast into the pool at `slots`. Rows of negative position leave their q as it was (a new q is
     zeroed)."""
+    if q is not None:
+        rc = (_calls or _bound()).paged_write(fmt, proj, pool, slots, positions, q_heads, float(theta), q)
+        if rc is not None:
+            return q if rc == 0 else _check(rc)
     p = _pool(fmt, pool)
     _need_cuda(proj)
     if proj.dtype != torch.float32 or proj.dim() != 2 or (proj.stride(1) != 1 and proj.shape[1] > 1):
@@ -783,6 +791,10 @@ def paged_write(fmt, proj, pool, slots, positions, q_heads, theta, q=None):
 def paged_read(fmt, pool, slots, k=None, v=None, dtype=torch.bfloat16):
     """amxfp4_paged_read: keys and values at `slots`, dequantized: two tensors [rows, kv_heads, head_dim], BF16 or float32; zeros for
     slots outside the pool."""
+    if k is not None and v is not None:
+        rc = (_calls or _bound()).paged_read(fmt, pool, slots, k, v)
+        if rc is not None:
+            return (k, v) if rc == 0 else _check(rc)
     p = _pool(fmt, pool)
     _here(slots)
     _ints(None, slots)
@@ -806,6 +818,10 @@ def paged_attention(fmt, q, pool, table, lens, starts, positions, scale, max_key
     """amxfp4_paged_attention: q BF16 [rows, q_heads, head_dim] against what the rows' sequences hold in the pool (lens, starts
     and positions out of paged_plan()). max_keys: at least the longest sequence, 0 if not known. Returns BF16 [rows, q_heads *
     head_dim]; rows behind the last sequence's are left as they were (zeros in a new tensor)."""
+    if out is not None and workspace is not None:
+        rc = (_calls or _bound()).paged_attention(fmt, q, pool, table, lens, starts, positions, float(scale), max_keys, out, workspace)
+        if rc is not None:
+            return out if rc == 0 else _check(rc)
     p = _pool(fmt, pool)
     _here(q, table, lens, starts, positions)
     if q.dtype != torch.bfloat16 or q.dim() != 3 or q.shape[2] != p.head_dim:

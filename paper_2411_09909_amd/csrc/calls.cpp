@@ -10,6 +10,7 @@
 #include <c10/hip/HIPStream.h>
 
 #include "../../include/amxfp4.h"
+#include "../../include/amxfp4_paged.h"
 
 namespace {
 
@@ -25,10 +26,15 @@ struct {
   decltype(&amxfp4_attention) attention;
   decltype(&amxfp4_attention_merged) attention_merged;
   decltype(&amxfp4_attention_decode) attention_decode;
+  decltype(&amxfp4_paged_plan) paged_plan;
+  decltype(&amxfp4_paged_write) paged_write;
+  decltype(&amxfp4_paged_read) paged_read;
+  decltype(&amxfp4_paged_attention) paged_attention;
 } entry;
 constexpr const char* kEntries[] = {"amxfp4_quantize", "amxfp4_quantize_scaled", "amxfp4_quantize_batched", "amxfp4_tensor_scale",
                                     "amxfp4_gemm", "amxfp4_gemm_scaled", "amxfp4_gemm_prepared", "amxfp4_attention",
-                                    "amxfp4_attention_merged", "amxfp4_attention_decode"};
+                                    "amxfp4_attention_merged", "amxfp4_attention_decode", "amxfp4_paged_plan", "amxfp4_paged_write",
+                                    "amxfp4_paged_read", "amxfp4_paged_attention"};
 constexpr size_t kNumEntries = sizeof(kEntries) / sizeof(kEntries[0]);
 static_assert(sizeof(entry) == kNumEntries * sizeof(void*), "one name per entry point");
 
@@ -231,6 +237,140 @@ PyObject* attention_decode(PyObject*, PyObject* const* args, Py_ssize_t n) try {
   Py_RETURN_NONE;
 }
 
+// ---- the paged cache: contiguous tensors on the current device, as binding.py's general way wants them
+
+const at::Tensor* here(PyObject* o) {
+  const at::Tensor* t = tensor(o);
+  return t && t->is_contiguous() && t->get_device() == c10::hip::current_device() ? t : nullptr;
+}
+
+// one-dimensional int32 of n elements (any number for n < 0)
+int32_t* ints(PyObject* o, int64_t n, int64_t* count = nullptr) {
+  const at::Tensor* t = here(o);
+  if (!t || t->scalar_type() != at::kInt || t->dim() != 1 || (n >= 0 && t->numel() != n)) return nullptr;
+  if (count) *count = t->numel();
+  return static_cast<int32_t*>(t->data_ptr());
+}
+
+// int32 [seqs, max_pages]
+int32_t* block_table(PyObject* o, int64_t seqs, int64_t& max_pages) {
+  const at::Tensor* t = here(o);
+  if (!t || t->scalar_type() != at::kInt || t->dim() != 2 || t->size(0) != seqs) return nullptr;
+  max_pages = t->size(1);
+  return static_cast<int32_t*>(t->data_ptr());
+}
+
+// four uint8 tensors as in binding.PagedPool
+bool pool(PyObject* o, const amx_format_t& f, amx_paged_pool_t& p) {
+  if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) return false;
+  const at::Tensor* t[4];
+  for (int i = 0; i < 4; ++i)
+    if (!(t[i] = here(PyTuple_GET_ITEM(o, i))) || t[i]->scalar_type() != at::kByte) return false;
+  if (t[0]->dim() != 4 || t[2]->sizes() != t[0]->sizes() || t[3]->sizes() != t[1]->sizes() || t[1]->dim() != (f.asymmetric ? 5 : 4)) return false;
+  const at::Tensor &c = *t[0], &s = *t[1];
+  if (s.size(0) != c.size(0) || s.size(1) != c.size(1) || s.size(2) != c.size(3) / 16 || s.size(3) != c.size(2) ||
+      (f.asymmetric && s.size(4) != 2) || c.size(1) > INT32_MAX || c.size(2) > INT32_MAX || c.size(3) > INT32_MAX / 2)
+    return false;
+  p = {c.size(0), (int32_t)c.size(2), (int32_t)c.size(1), (int32_t)c.size(3) * 2, 0, bytes(t[0]), bytes(t[1]), bytes(t[2]), bytes(t[3])};
+  return true;
+}
+
+bool integer(PyObject* o, int64_t& v) {
+  if (!PyLong_CheckExact(o)) return false;
+  v = PyLong_AsLongLong(o);
+  if (v == -1 && PyErr_Occurred()) {
+    PyErr_Clear();
+    return false;
+  }
+  return true;
+}
+
+// paged_plan(lens, new_rows, table, queue, state, page_size, (lens, starts, slots, positions, state))
+PyObject* paged_plan(PyObject*, PyObject* const* args, Py_ssize_t n) try {
+  if (n != 7 || !PyTuple_Check(args[6]) || PyTuple_GET_SIZE(args[6]) != 5) Py_RETURN_NONE;
+  int64_t seqs, pages, max_pages, page_size, rows;
+  int32_t *lens, *fresh, *table, *queue, *state, *out[5];
+  if (!(lens = ints(args[0], -1, &seqs)) || !(fresh = ints(args[1], seqs)) || !(table = block_table(args[2], seqs, max_pages)) ||
+      !(queue = ints(args[3], -1, &pages)) || !(state = ints(args[4], 4)) || !integer(args[5], page_size) ||
+      !(out[2] = ints(PyTuple_GET_ITEM(args[6], 2), -1, &rows)))
+    Py_RETURN_NONE;
+  const int64_t want[5] = {seqs, seqs + 1, rows, rows, 4};
+  for (int i = 0; i < 5; ++i)
+    if (!(out[i] = ints(PyTuple_GET_ITEM(args[6], i), want[i]))) Py_RETURN_NONE;
+  return run([&](void* s) {
+    return entry.paged_plan(lens, fresh, seqs, rows, page_size, pages, max_pages, state, queue, table, out[0], out[1], out[2], out[3], out[4], s);
+  });
+} catch (const std::exception&) {
+  Py_RETURN_NONE;
+}
+
+// paged_write(fmt, proj, pool, slots, positions, q_heads, theta, q)
+PyObject* paged_write(PyObject*, PyObject* const* args, Py_ssize_t n) try {
+  amx_format_t f;
+  amx_paged_pool_t p;
+  const at::Tensor *x, *q;
+  int64_t heads;
+  if (n != 8 || !format(args[0], f) || !(x = tensor(args[1])) || !pool(args[2], f, p) || !integer(args[5], heads) || !PyFloat_CheckExact(args[6]) ||
+      !(q = here(args[7])))
+    Py_RETURN_NONE;
+  if (x->scalar_type() != at::kFloat || x->dim() != 2 || x->stride(1) != 1 || x->get_device() != c10::hip::current_device() ||
+      q->scalar_type() != at::kBFloat16 || heads <= 0 || heads > 1024)
+    Py_RETURN_NONE;
+  const int64_t rows = x->size(0), width = (heads + 2 * (int64_t)p.kv_heads) * p.head_dim, ld = rows > 1 ? x->stride(0) : width;
+  int32_t *slots = ints(args[3], rows), *positions = ints(args[4], rows);
+  if (!slots || !positions || x->size(1) < width || q->numel() != rows * heads * p.head_dim) Py_RETURN_NONE;
+  const float* in = static_cast<const float*>(x->data_ptr());
+  const double theta = PyFloat_AS_DOUBLE(args[6]);
+  void* to = q->data_ptr();
+  return run([&](void* s) { return entry.paged_write(&f, &p, in, rows, ld, heads, slots, positions, theta, to, s); });
+} catch (const std::exception&) {
+  Py_RETURN_NONE;
+}
+
+// paged_read(fmt, pool, slots, k, v)
+PyObject* paged_read(PyObject*, PyObject* const* args, Py_ssize_t n) try {
+  amx_format_t f;
+  amx_paged_pool_t p;
+  const at::Tensor *k, *v;
+  int64_t rows;
+  if (n != 5 || !format(args[0], f) || !pool(args[1], f, p) || !(k = here(args[3])) || !(v = here(args[4]))) Py_RETURN_NONE;
+  int32_t* slots = ints(args[2], -1, &rows);
+  const bool bf16 = k->scalar_type() == at::kBFloat16;
+  if (!slots || (!bf16 && k->scalar_type() != at::kFloat) || v->scalar_type() != k->scalar_type() || k->dim() != 3 || v->sizes() != k->sizes() ||
+      k->size(0) != rows || k->size(1) != p.kv_heads || k->size(2) != p.head_dim)
+    Py_RETURN_NONE;
+  void *to_k = k->data_ptr(), *to_v = v->data_ptr();
+  return run([&](void* s) { return entry.paged_read(&f, &p, slots, rows, bf16, to_k, to_v, s); });
+} catch (const std::exception&) {
+  Py_RETURN_NONE;
+}
+
+// paged_attention(fmt, q, pool, table, lens, starts, positions, scale, max_keys, out, workspace)
+PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n) try {
+  amx_format_t f;
+  amx_paged_pool_t p;
+  const at::Tensor *q, *out, *ws;
+  int64_t seqs, max_pages, max_keys;
+  if (n != 11 || !format(args[0], f) || !(q = here(args[1])) || !pool(args[2], f, p) || !PyFloat_CheckExact(args[7]) || !integer(args[8], max_keys) ||
+      !(out = here(args[9])) || !(ws = here(args[10])))
+    Py_RETURN_NONE;
+  int32_t *lens = ints(args[4], -1, &seqs), *table, *starts, *positions;
+  if (!lens || q->scalar_type() != at::kBFloat16 || q->dim() != 3 || q->size(2) != p.head_dim || out->scalar_type() != at::kBFloat16 ||
+      out->numel() != q->numel() || !(table = block_table(args[3], seqs, max_pages)) || !(starts = ints(args[5], seqs + 1)) ||
+      !(positions = ints(args[6], q->size(0))))
+    Py_RETURN_NONE;
+  const int64_t rows = q->size(0), heads = q->size(1);
+  const float scale = (float)PyFloat_AS_DOUBLE(args[7]);
+  const void* from = q->data_ptr();
+  void *to = out->data_ptr(), *scratch = ws->data_ptr();
+  const size_t ws_bytes = size_of(ws);
+  return run([&](void* s) {
+    return entry.paged_attention(&f, &p, from, rows, heads, table, seqs, max_pages, lens, starts, positions, scale, max_keys, to, scratch, ws_bytes, s);
+  });
+} catch (const std::exception&) {
+  Py_RETURN_NONE;
+}
+
 // bind(class of the formats, address of each of `entries`)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
   void* address[kNumEntries];
@@ -250,7 +390,8 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 #define CALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {CALL(quantize), CALL(quantize_batched), CALL(tensor_scale), CALL(gemm), CALL(gemm_prepared),
-                          CALL(attention), CALL(attention_decode), CALL(bind), {nullptr, nullptr, 0, nullptr}};
+                          CALL(attention), CALL(attention_decode), CALL(paged_plan), CALL(paged_write), CALL(paged_read),
+                          CALL(paged_attention), CALL(bind), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

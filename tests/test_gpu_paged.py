@@ -455,6 +455,35 @@ def test_on_another_stream():
         assert torch.equal(a.out, b.out) and torch.equal(a.lens, b.lens)
 
 
+def test_the_native_way_and_the_general_one(monkeypatch):
+    """With all buffers given the calls go through the native module, and give what the general way gives."""
+    fmt = binding.make_format()
+    a, b = (Server(fmt, 4, 2, 128, 3, 4, 20, 16, 30) for _ in range(2))
+    b.queue.copy_(a.queue)
+    b.pool = binding.PagedPool(*(t.clone() for t in a.pool))
+    taken = []
+
+    class Spy:
+        def __getattr__(self, name):
+            def call(*args):
+                rc = getattr(calls, name)(*args)
+                taken.append((name, rc))
+                return rc
+            return call
+    binding.load()
+    calls = binding._calls
+    for s, module in ((a, Spy()), (b, binding._GeneralWay())):
+        monkeypatch.setattr(binding, "_calls", module)
+        s.proj.copy_(torch.arange(s.proj.numel(), device="cuda").view_as(s.proj) % 37 - 15.5)
+        s.new.copy_(dev([9, 1, 5]))
+        s.step()
+        k = torch.zeros(30, 2, 128, dtype=torch.bfloat16, device="cuda")
+        s.kv = binding.paged_read(fmt, s.pool, s.plan.slots, k=k, v=k.clone())
+    assert taken == [("paged_plan", 0), ("paged_write", 0), ("paged_attention", 0), ("paged_read", 0)]
+    for x, y in zip((a.out, a.q, a.table, a.queue, *a.plan, *a.pool, *a.kv), (b.out, b.q, b.table, b.queue, *b.plan, *b.pool, *b.kv)):
+        assert torch.equal(x, y)
+
+
 def test_binding_refuses_what_does_not_fit():
     fmt = binding.make_format()
     s = Server(fmt, 4, 2, 64, 3, 4, 20, 16, 30)
