@@ -6,22 +6,24 @@
 // group g of the keys alone (the query's other groups are zeros there), so that the group's scales, which are those of a token,
 // can be applied to the product: s[c][j] = sum_g S[j][g] (q . elements)[c][j][g]. The keys' elements are converted to BF16, which
 // holds them, and not scaled.
-//   sign pair   S_p q.e+ + S_n q.e- = (S_p + S_n) / 2 q.e + (S_p - S_n) / 2 q.|e|: two products, |e| by clearing sign bits. In FP32;
-//               what cancels is 2^-23 of the larger scale's share.
+//   sign pair   S_p q.e+ + S_n q.e- = S_n q.e + (S_p - S_n) q.e+: two products, in FP32; what cancels is 2^-23 of the larger
+//               scale's share.
 //   (The codes as they are on the block-scaled instruction, the query as two E4M3 parts, saves the conversion and costs
 //   exactness: that instruction adds its products in a window of 2^-13 of the largest, and a score was off by 2^-12 of it.)
 // Values. The codes of 64 tokens are transposed by ds_read_b64_tr_b4 (16 lanes read 16 rows of 16 codes and get one column
 // each), converted to BF16 elements and multiplied with p[c][j] S[j][g], rounded to BF16: O[d][c] = sum_j (p S)[j][c] e[j][d].
-// The two sign classes stay apart here (e+ with p S_p, e- with p S_n): with (S_p + S_n) / 2 and (S_p - S_n) / 2 the rounding of the
-// larger class's weight would drown a smaller one. The columns of the other groups compute products nobody reads.
+// The two sign classes stay apart here (e+ with p S_p, e- with p S_n): with p S_n and p (S_p - S_n) the rounding of a much
+// larger S_n would drown the positive class. The columns of the other groups compute products nobody reads.
 // Layout of a tile of 64 tokens in a wave: lane (column or row r = l % 16, quarter u = l / 16). S^T comes out of the matrix
 // instruction t (of 4) with tile rows 4 u + i in lane (r, u): those rows are keys 16 u + 4 t + i, so that a lane holds the 16 keys
 // 16 u .. of its column, in the order in which the second product wants them, and needs the scales of 16 neighbouring tokens, 32 bytes.
 //
-// Division of the work: units of 64 tokens of one sequence, key head and tile of combinations, in that order, dealt out
-// evenly over the workgroups, whatever the sequences' lengths are. Every workgroup finds its own range from the lengths (a prefix sum
-// over the sequences, in LDS). A range may begin and end within a sequence: those partial results (O, m, l) go to the
-// workspace, at most two to a workgroup, and paged_attention_join_kernel adds them up.
+// Division of the work, by the host's rules at the end of this file:
+//   split    units of 64 tokens (more where there could be 2^31 of them) of one sequence, key head and tile of combinations, in
+//            that order, are dealt out evenly over the workgroups, whatever the sequences' lengths are. Every workgroup finds its own
+//            range from the lengths (a prefix sum over the sequences, in LDS). A range may begin and end within a sequence: those
+//            partial results (O, m, l) go to the workspace, at most two to a workgroup, and paged_attention_join_kernel adds them up.
+//   whole    short sequences: a sequence and key head to a workgroup or, where there are many, to a wave, with all its tokens.
 #include "paged.h"
 
 #include "kernels.h"
@@ -41,43 +43,31 @@ typedef short i16x2 __attribute__((ext_vector_type(2)));
 constexpr int kTile = 64;        // tokens of a unit
 constexpr int kMostGroups = 1024;  // workgroups
 
-// What one launch reads.
+// What one launch reads, beside the arrays of the sequences.
 struct PagedWork {
   const uint16_t* q;
-  const int32_t *table, *lens, *starts, *positions;
   uint16_t* out;
   uint8_t* workspace;
   int64_t rows, max_pages;
   int seqs, q_heads, per;  // per: query heads to a key head
   float scale_log2;
-  int whole;  // a unit is a sequence, key head and tile of combinations with all its tokens
+  int whole, unit_log2;    // tiles of 64 tokens to a unit
 };
 
 // What a workgroup leaves behind for the joining kernel, at the front of the workspace.
 struct PagedTail {
-  uint64_t units, end;    // all units; one past the last of the sequence, key head and tile that this workgroup began and did not end
+  uint32_t units, end;    // all units; one past the last of the sequence, key head and tile that this workgroup began and did not end
   uint32_t groups, owner;  // workgroups among which the units are divided; 1: it began such a one
   int32_t seq, head, tile, pad;
 };
 
 // units of a workgroup: [first_unit(g), first_unit(g + 1))
-__device__ __forceinline__ uint64_t first_unit(uint64_t units, uint32_t groups, uint32_t g) {
-  return units / groups * g + (uint64_t)((units % groups) * g / groups);
+__device__ __forceinline__ uint32_t first_unit(uint32_t units, uint32_t groups, uint32_t g) {
+  return units / groups * g + (units % groups) * g / groups;  // (groups <= 1024)
 }
 
 template <int NC, int D>
 constexpr int kPartFloats = NC * (D + 2);
-
-__device__ __forceinline__ uint32_t divide(uint64_t a, uint64_t b, uint64_t& rest) {
-  if (((a | b) >> 32) == 0) {
-    const uint32_t q = (uint32_t)a / (uint32_t)b;
-    rest = (uint32_t)a - q * (uint32_t)b;
-    return q;
-  }
-  const uint64_t q = a / b;
-  rest = a - q * b;
-  return (uint32_t)q;
-}
 
 // A sequence as the units see it. NT: tiles of tokens (one at least, so that a row without keys is written), CT: tiles of combinations.
 struct PagedSequence {
@@ -85,13 +75,14 @@ struct PagedSequence {
   uint32_t rows, keys, NT, CT;
 };
 template <int NC>
-__device__ __forceinline__ PagedSequence paged_sequence(const PagedWork& w, const PagedPool& pool, int b) {
+__device__ __forceinline__ PagedSequence paged_sequence(const PagedWork& w, uint32_t page_log2, const int32_t* __restrict__ lens,
+                                                        const int32_t* __restrict__ starts, int b) {
   PagedSequence s;
-  const int64_t a = max((int64_t)w.starts[b], (int64_t)0), e = min((int64_t)w.starts[b + 1], w.rows);
-  const int64_t n = w.lens[b];
+  const int64_t a = max((int64_t)starts[b], (int64_t)0), e = min((int64_t)starts[b + 1], w.rows);
+  const int n = lens[b];
   s.first = a;
   s.rows = e > a ? (uint32_t)(e - a) : 0u;
-  s.keys = (uint32_t)max((int64_t)0, min(n, w.max_pages << pool.page_log2));
+  s.keys = (uint32_t)max(0, min(n, (int)(w.max_pages << page_log2)));  // (at most 2^30)
   s.NT = max((s.keys + kTile - 1) / kTile, 1u);
   s.CT = (uint32_t)(((uint64_t)s.rows * w.per + NC - 1) / NC);
   return s;
@@ -144,6 +135,27 @@ __device__ __forceinline__ u32x4 elements(uint32_t word) {
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, 1.0f, 3))};
 }
 
+// The elements of one sign class, zeros for the others: as 16-bit integers negative numbers lie below 0. (The words one by one, through
+// a variable: a bit cast of a vector's element itself takes element 0.)
+__device__ __forceinline__ u32x4 positive(u32x4 e) {
+  u32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t two = e[i];
+    v[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(i16x2, two), (i16x2{0, 0})));
+  }
+  return v;
+}
+__device__ __forceinline__ u32x4 negative(u32x4 e) {
+  u32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t two = e[i];
+    v[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(i16x2, two), (i16x2{0, 0})));
+  }
+  return v;
+}
+
 template <int SCALE_KIND, bool ASYM, int D, int GC>
 struct PagedTile {
   static constexpr int kGroups = D / 32, GS = kGroups / GC;
@@ -154,98 +166,107 @@ struct PagedTile {
   uint32_t bad;  // sub-blocks of 16 tokens whose page is none
 };
 
-template <int SCALE_KIND, bool ASYM, int D, int GC>
-__global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void paged_attention_kernel(PagedPool pool, PagedWork w) {
+// SHARE: waves to a sequence and key head, 4 or 1.
+template <int SCALE_KIND, bool ASYM, int D, int GC, int SHARE>
+__global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void paged_attention_kernel(
+    PagedPool pool, PagedWork w, const int32_t* __restrict__ table, const int32_t* __restrict__ lens, const int32_t* __restrict__ starts,
+    const int32_t* __restrict__ positions) {
   using Tile = PagedTile<SCALE_KIND, ASYM, D, GC>;
   constexpr int GS = Tile::GS, NC = 16 / GC, DT = D / 16;
   constexpr int kValueBytes = kTile * D / 2;  // of a wave's tile of V
   constexpr int kShareFloats = NC * D;
   extern __shared__ __align__(16) uint8_t lds[];
-  uint64_t* ends = reinterpret_cast<uint64_t*>(lds);  // units up to and with a sequence
-  uint8_t* region = lds + (((size_t)w.seqs * 8 + 15) & ~(size_t)15);
-  __shared__ uint64_t edge[4];
   __shared__ float top_of[4][NC], sum_of[4][NC];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, u = lane >> 4, c = r / GC, gc = r % GC;
+  uint32_t* const ends = reinterpret_cast<uint32_t*>(lds);  // split: units up to and with a sequence
+  uint8_t* const region = lds + (w.whole ? 0 : ((size_t)w.seqs * 4 + 15) & ~(size_t)15);
   uint8_t* const mine = region + wave * kValueBytes;
 
-  // ---- the workgroup's range of units
-  {
+  int b, head;
+  uint32_t ct = 0, unit = 0, hi = 0;
+  if (SHARE == 1 || w.whole) {
+    const uint32_t which = SHARE == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
+    if (which >= (uint32_t)w.seqs * pool.kv_heads) return;  // (SHARE == 1: the wave; nobody waits for it)
+    b = __builtin_amdgcn_readfirstlane((int)(which / pool.kv_heads)), head = (int)which - b * (int)pool.kv_heads;
+    ct = blockIdx.y;
+  } else {
+    // ---- the workgroup's range of units. The sums stay at kMostUnits once they reach it, which only rows that sequences share
+    // can bring about: then units are missing, but each is one of its sequence's.
+    constexpr uint32_t kMostUnits = 0x7FFFFFFF;
+    __shared__ uint32_t edge[4];
     const int each = (w.seqs + 255) >> 8, b0 = threadIdx.x * each, b1 = min(w.seqs, b0 + each);
-    uint64_t sum = 0;
-    for (int b = b0; b < b1; ++b) {
-      const PagedSequence s = paged_sequence<NC>(w, pool, b);
-      sum += (uint64_t)pool.kv_heads * s.CT * (w.whole ? 1 : s.NT);
-      ends[b] = sum;
+    uint32_t sum = 0;
+    for (int i = b0; i < b1; ++i) {
+      const PagedSequence s = paged_sequence<NC>(w, pool.page_log2, lens, starts, i);
+      const uint64_t mine = min((uint64_t)s.CT * ((s.NT + (1u << w.unit_log2) - 1) >> w.unit_log2), (uint64_t)kMostUnits) * pool.kv_heads;
+      ends[i] = sum = (uint32_t)min(sum + mine, (uint64_t)kMostUnits);
     }
-    uint64_t upto = sum;
+    uint32_t upto = sum;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-      const uint64_t v = __shfl_up(upto, o, 64);
-      if (lane >= o) upto += v;
+      const uint32_t v = __shfl_up(upto, o, 64);
+      if (lane >= o) upto = min(upto + v, kMostUnits);
     }
     if (lane == 63) edge[wave] = upto;
     __syncthreads();
-    uint64_t before = upto - sum;
-    for (int i = 0; i < wave; ++i) before += edge[i];
-    for (int b = b0; b < b1; ++b) ends[b] += before;
+    uint32_t before = __shfl_up(upto, 1, 64);
+    if (lane == 0) before = 0;
+    for (int i = 0; i < wave; ++i) before = min(before + edge[i], kMostUnits);
+    for (int i = b0; i < b1; ++i) ends[i] = min(ends[i] + before, kMostUnits);
     __syncthreads();
-  }
-  const uint64_t units = ends[w.seqs - 1];
-  const uint64_t busy = w.whole ? units : (units + 3) / 4;  // a tile to each wave at least
-  const uint32_t groups = (uint32_t)max((uint64_t)1, min((uint64_t)gridDim.x, busy)), g = blockIdx.x;
-  PagedTail* tail = reinterpret_cast<PagedTail*>(w.workspace) + g;
-  if (threadIdx.x == 0 && !w.whole) *tail = PagedTail{units, 0, groups, 0, 0, 0, 0, 0};
-  if (g >= groups || units == 0) return;
-  const uint64_t lo = first_unit(units, groups, g), hi = first_unit(units, groups, g + 1);
-  int b = 0;
-  for (int step = w.seqs; step > 0;) {  // the first sequence whose units end behind lo
-    const int half = step >> 1, mid = b + half;
-    if (ends[mid] <= lo)
-      b = mid + 1, step -= half + 1;
-    else
-      step = half;
+    const uint32_t units = __builtin_amdgcn_readfirstlane(ends[w.seqs - 1]);
+    // a tile to each wave at least
+    const uint32_t groups = max(1u, min((uint32_t)gridDim.x, w.unit_log2 ? units : (units + 3) / 4)), g = blockIdx.x;
+    if (threadIdx.x == 0) reinterpret_cast<PagedTail*>(w.workspace)[g] = PagedTail{units, 0, groups, 0, 0, 0, 0, 0};
+    if (g >= groups || units == 0) return;
+    unit = first_unit(units, groups, g), hi = first_unit(units, groups, g + 1);
+    // the first sequence whose units end behind the range's first: its 64th of the sequences, then in there
+    const int part = (w.seqs + 63) >> 6;
+    const int chunk = (int)__popcll(__builtin_amdgcn_ballot_w64(ends[min((lane + 1) * part, w.seqs) - 1] <= unit));
+    const int at = chunk * part + lane;
+    b = chunk * part + (int)__popcll(__builtin_amdgcn_ballot_w64(lane < part && at < w.seqs && ends[min(at, w.seqs - 1)] <= unit));
+    head = 0;
   }
 
-  for (uint64_t unit = lo; unit < hi;) {
-    while (ends[b] <= unit) ++b;
-    const PagedSequence s = paged_sequence<NC>(w, pool, b);
-    const uint64_t base = b ? ends[b - 1] : 0;
-    uint64_t tile64, ct64;
-    const uint32_t NT = w.whole ? 1 : s.NT;
-    const uint32_t seg = divide(unit - base, NT, tile64);
-    const uint32_t head = divide(seg, s.CT, ct64), ct = (uint32_t)ct64;
-    const uint32_t t0 = (uint32_t)tile64;
-    const uint64_t after = base + ((uint64_t)seg + 1) * NT;  // the unit behind this segment's last
-    const uint32_t t1 = w.whole ? s.NT : (uint32_t)min((uint64_t)NT, t0 + (hi - unit));
-    const int32_t* row_table = w.table + (int64_t)b * w.max_pages;
+  for (;;) {
+    uint32_t t0 = 0, t1, after = 0;  // tiles of tokens; the unit behind the segment's last
+    bool complete = true;
+    if (SHARE == 4 && !w.whole)
+      while (__builtin_amdgcn_readfirstlane(ends[b]) <= unit) ++b;
+    const PagedSequence s = paged_sequence<NC>(w, pool.page_log2, lens, starts, b);
+    if (SHARE == 1 || w.whole) {
+      if (ct >= s.CT) return;
+      t1 = s.NT;
+    } else {
+      const uint32_t base = b ? __builtin_amdgcn_readfirstlane(ends[b - 1]) : 0u;
+      const uint32_t per_segment = (s.NT + (1u << w.unit_log2) - 1) >> w.unit_log2;
+      const uint32_t seg = (unit - base) / per_segment, first = (unit - base) - seg * per_segment;
+      head = (int)(seg / s.CT), ct = seg - (uint32_t)head * s.CT;
+      after = base + (seg + 1) * per_segment;
+      const uint32_t end = min(per_segment, first + (hi - unit));
+      t0 = first << w.unit_log2, t1 = min(s.NT, end << w.unit_log2);
+      complete = first == 0 && end == per_segment;
+      unit += end - first;
+    }
+    t0 = __builtin_amdgcn_readfirstlane(t0), t1 = __builtin_amdgcn_readfirstlane(t1);
+    ct = __builtin_amdgcn_readfirstlane(ct), head = __builtin_amdgcn_readfirstlane(head);
+    const int32_t* row_table = table + (int64_t)b * w.max_pages;
     const uint32_t last_entry = (uint32_t)(w.max_pages - 1);
-
-    // ---- this lane's combination
-    const uint64_t combination = (uint64_t)ct * NC + c;
-    const bool asked = combination < (uint64_t)s.rows * w.per;
-    const uint32_t row_of = asked ? (uint32_t)(combination / (uint32_t)w.per) : 0u, head_of = asked ? (uint32_t)(combination % (uint32_t)w.per) : 0u;
-    const int64_t row = s.first + row_of;
-    // tokens it sees; columns that nobody asked for see all and are not looked at
-    const int limit = asked ? min(max(w.positions[row], -1) + 1, (int)s.keys) : 0x7FFFFFFF;
-    int least = limit, most = asked ? limit : 0;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) least = min(least, __shfl_xor(least, o, 64)), most = max(most, __shfl_xor(most, o, 64));
-    least = __builtin_amdgcn_readfirstlane(least), most = __builtin_amdgcn_readfirstlane(most);
-    const uint32_t stop = min(t1, (uint32_t)(most + kTile - 1) / kTile);
 
     // ---- requests
     const int64_t page_stride = (int64_t)pool.kv_heads << pool.page_log2;
+    uint32_t id[4];  // pages of the four sub-blocks of 16 tokens of the tile that is requested next
+    auto look_up = [&](uint32_t tile) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) id[k] = (uint32_t)row_table[min((tile * kTile + 16 * k) >> pool.page_log2, last_entry)];
+    };
     auto request = [&](uint32_t tile, Tile& d) {
-      uint32_t id[4];
       d.bad = 0;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint32_t entry = min((tile * kTile + 16 * k) >> pool.page_log2, last_entry);
-        id[k] = (uint32_t)__builtin_amdgcn_readfirstlane(row_table[entry]);
+      for (int k = 0; k < 4; ++k)
         if (id[k] >= pool.pages) d.bad |= 1u << k, id[k] = 0;
-      }
       const uint32_t mask = (1u << pool.page_log2) - 1;
       auto pick = [&](int k) {  // the id of a sub-block that depends on the lane
         const uint32_t a = k & 1 ? id[1] : id[0], z = k & 1 ? id[3] : id[2];
@@ -262,31 +283,45 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
 #pragma unroll
         for (int t = 0; t < Tile::NK; ++t) d.k[t] = *reinterpret_cast<const u32x4*>(p + t * (D == 64 ? 8 : 4) * (D / 2));
       }
-#pragma unroll
-      for (int n = 0; n < Tile::NV; ++n) {
-        constexpr int kParts = D / 32;  // pieces of 16 bytes in a row
-        const uint32_t at = n * (64 / kParts) + lane / kParts, token = tile * kTile + at;
-        const uint32_t page = D == 128 ? id[n] : (lane < 32 ? id[2 * n & 3] : id[(2 * n + 1) & 3]);
-        d.v[n] = *reinterpret_cast<const u32x4*>(pool.v_codes + first_token(page, token) * (D / 2) + 16 * (lane % kParts));
-      }
       // scales of tokens 16 u .. of group s * GC + gc
-      {
-        const uint32_t token = (tile * kTile + 16 * u) & mask;
-        const int64_t at = (((int64_t)pick(u) * pool.kv_heads + head) * Tile::kGroups + gc) << pool.page_log2;
-        const int64_t offset = (at + token) * (ASYM ? 2 : 1);
+      const uint32_t place = (tile * kTile + 16 * u) & mask;
+      const int64_t at = (((int64_t)pick(u) * pool.kv_heads + head) * Tile::kGroups + gc) << pool.page_log2;
+      const int64_t offset = (at + place) * (ASYM ? 2 : 1);
+      auto scales = [&](const uint8_t* from, u32x4 (&to)[GS][Tile::kScaleWords / 4]) {
 #pragma unroll
         for (int st = 0; st < GS; ++st)
 #pragma unroll
-          for (int i = 0; i < Tile::kScaleWords / 4; ++i) {
-            const int64_t o = offset + (((int64_t)st * GC) << pool.page_log2) * (ASYM ? 2 : 1) + 16 * i;
-            d.ks[st][i] = *reinterpret_cast<const u32x4*>(pool.k_scales + o);
-            d.vs[st][i] = *reinterpret_cast<const u32x4*>(pool.v_scales + o);
-          }
+          for (int i = 0; i < Tile::kScaleWords / 4; ++i)
+            to[st][i] = *reinterpret_cast<const u32x4*>(from + offset + (((int64_t)st * GC) << pool.page_log2) * (ASYM ? 2 : 1) + 16 * i);
+      };
+      scales(pool.k_scales, d.ks);
+#pragma unroll
+      for (int n = 0; n < Tile::NV; ++n) {
+        constexpr int kParts = D / 32;  // pieces of 16 bytes in a row
+        const uint32_t token = tile * kTile + n * (64 / kParts) + lane / kParts;
+        const uint32_t page = D == 128 ? id[n] : (lane < 32 ? id[2 * n & 3] : id[(2 * n + 1) & 3]);
+        d.v[n] = *reinterpret_cast<const u32x4*>(pool.v_codes + first_token(page, token) * (D / 2) + 16 * (lane % kParts));
       }
+      scales(pool.v_scales, d.vs);
     };
     Tile next;
-    uint32_t tile = t0 + wave;
-    if (tile < stop) request(tile, next);
+    uint32_t tile = t0 + (SHARE == 1 ? 0 : wave);
+    look_up(tile);
+    if (tile < t1) request(tile, next);
+    look_up(tile + SHARE);
+
+    // ---- this lane's combination
+    const uint64_t combination = (uint64_t)ct * NC + c;
+    const bool asked = combination < (uint64_t)s.rows * w.per;
+    const uint32_t row_of = asked ? (uint32_t)(combination / (uint32_t)w.per) : 0u, head_of = asked ? (uint32_t)(combination % (uint32_t)w.per) : 0u;
+    const int64_t row = s.first + row_of;
+    // tokens it sees; columns that nobody asked for see all and are not looked at
+    const int limit = asked ? min(max(positions[row], -1) + 1, (int)s.keys) : 0x7FFFFFFF;
+    int least = limit, most = asked ? limit : 0;  // (the same in all quarters and in the columns of a combination)
+#pragma unroll
+    for (int o = GC; o < 16; o <<= 1) least = min(least, __shfl_xor(least, o, 64)), most = max(most, __shfl_xor(most, o, 64));
+    least = __builtin_amdgcn_readfirstlane(least), most = __builtin_amdgcn_readfirstlane(most);
+    const uint32_t stop = min(t1, (uint32_t)(most + kTile - 1) / kTile);
 
     // ---- the query: dimensions 32 j + 8 u .. of group j, zeros where the column is not the group's
     u32x4 q[Tile::kGroups];
@@ -302,9 +337,9 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i] = f32x4{0, 0, 0, 0};
     float m = -INFINITY, l = 0.f;
-    const float sc = ASYM ? 0.5f * w.scale_log2 : w.scale_log2;
+    const float sc = w.scale_log2;
 
-    for (; tile < stop; tile += 4) {
+    for (; tile < stop; tile += SHARE) {
       const Tile d = next;
       // V into LDS, piece p of row j at p ^ (some bits of j): rows that 16 lanes read at once lie in different banks
 #pragma unroll
@@ -313,7 +348,10 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
         const int j = n * (64 / kParts) + lane / kParts, part = (lane % kParts) ^ (D == 128 ? (j >> 2) & 3 : (j >> 3) & 1);
         *reinterpret_cast<u32x4*>(mine + j * (D / 2) + 16 * part) = d.v[n];
       }
-      if (tile + 4 < stop) request(tile + 4, next);
+      if (tile + SHARE < stop) {
+        request(tile + SHARE, next);
+        look_up(tile + 2 * SHARE);
+      }
 
       // ---- scores
       float x[16];
@@ -341,7 +379,7 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
             const u32x4 e = elements(kw[Tile::kGroups * t + j]);  // (heads of 64: two tiles' words in turn)
             const bf16x8 qj = __builtin_bit_cast(bf16x8, q[j]);
             dot = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, e), qj, dot, 0, 0, 0);
-            if constexpr (ASYM) with = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, e & 0x7FFF7FFFu), qj, with, 0, 0, 0);
+            if constexpr (ASYM) with = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, positive(e)), qj, with, 0, 0, 0);
           }
           if constexpr (ASYM) {
             const uint32_t s0 = d.ks[st][t >> 1][2 * t & 3], s1 = d.ks[st][t >> 1][(2 * t + 1) & 3];
@@ -349,7 +387,7 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
                                 two_scales<SCALE_KIND, true>(s1)};
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              x[4 * t + i] += __builtin_fmaf(a[i][0] + a[i][1], dot[i], (a[i][0] - a[i][1]) * with[i]);
+              x[4 * t + i] = __builtin_fmaf(a[i][1], dot[i], __builtin_fmaf(a[i][0] - a[i][1], with[i], x[4 * t + i]));
           } else {
             const uint32_t s0 = d.ks[st][0][t];
             const f32x2 a = two_scales<SCALE_KIND, false>(s0), z = two_scales<SCALE_KIND, true>(s0);
@@ -416,16 +454,8 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
           for (int h = 0; h < 2; ++h) {
             const u32x4 e = elements((uint32_t)codes[h]);
             if constexpr (ASYM) {
-              uint32_t pos[4], neg[4];  // as 16-bit integers negative numbers lie below 0
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const uint32_t two = e[i];  // (a bit cast of the vector's element itself takes element 0)
-                const i16x2 v = __builtin_bit_cast(i16x2, two), z = {0, 0};
-                pos[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(v, z));
-                neg[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(v, z));
-              }
-              o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, (u32x4{pos[0], pos[1], pos[2], pos[3]})), h ? p1 : p0, o[dt], 0, 0, 0);
-              o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, (u32x4{neg[0], neg[1], neg[2], neg[3]})), h ? n1 : n0, o[dt], 0, 0, 0);
+              o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, positive(e)), h ? p1 : p0, o[dt], 0, 0, 0);
+              o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, negative(e)), h ? n1 : n0, o[dt], 0, 0, 0);
             } else {
               o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, e), h ? p1 : p0, o[dt], 0, 0, 0);
             }
@@ -434,8 +464,23 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
       }
     }
 
-    // ---- the four waves' shares, each against its own maximum, become one
     l = quarters_sum(l);
+    if constexpr (SHARE == 1) {
+      const float inv = l > 0.f ? 1.0f / l : 0.f;
+      if (asked) {
+        uint16_t* to = w.out + (row * w.q_heads + (int64_t)head * w.per + head_of) * D + 4 * u;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+          if ((dt >> 1) % GC == gc) {
+            const f32x4 v = o[dt] * inv;
+            *reinterpret_cast<uint2*>(to + dt * 16) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+          }
+      }
+      ct += gridDim.y;
+      continue;
+    }
+
+    // ---- the four waves' shares, each against its own maximum, become one
     if (u == 0 && gc == 0) top_of[wave][c] = m, sum_of[wave][c] = l;
     __syncthreads();  // (and all waves have read their V)
     const float top = fmaxf(fmaxf(top_of[0][c], top_of[1][c]), fmaxf(top_of[2][c], top_of[3][c]));
@@ -445,11 +490,10 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
     for (int dt = 0; dt < DT; ++dt)
       if ((dt >> 1) % GC == gc) *reinterpret_cast<f32x4*>(share + wave * kShareFloats + c * D + dt * 16 + 4 * u) = o[dt] * factor;
     __syncthreads();
-    const bool complete = w.whole || (t0 == 0 && t1 == NT);
     float* part = nullptr;
     if (!complete)  // slot 0: begun by another workgroup, 1: begun here
       part = reinterpret_cast<float*>(w.workspace + (((size_t)gridDim.x * sizeof(PagedTail) + 255) & ~(size_t)255)) +
-             (2 * (size_t)g + (t0 == 0 ? 1 : 0)) * kPartFloats<NC, D>;
+             (2 * (size_t)blockIdx.x + (t0 == 0 ? 1 : 0)) * kPartFloats<NC, D>;
     for (int i = threadIdx.x; i < kShareFloats / 2; i += 256) {
       const int combo = 2 * i / D, dim = 2 * i % D;
       float2 v = *reinterpret_cast<const float2*>(share + 2 * i);
@@ -475,9 +519,16 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
         if (dim == 0) part[NC * D + combo] = best * sc, part[NC * D + NC + combo] = total;
       }
     }
-    if (!complete && t0 == 0 && threadIdx.x == 0) *tail = PagedTail{units, after, groups, 1, b, (int32_t)head, (int32_t)ct, 0};
+    if (w.whole) {
+      ct += gridDim.y;
+    } else {
+      if (!complete && t0 == 0 && threadIdx.x == 0) {
+        PagedTail* tail = reinterpret_cast<PagedTail*>(w.workspace) + blockIdx.x;
+        tail->end = after, tail->owner = 1, tail->seq = b, tail->head = head, tail->tile = (int32_t)ct;
+      }
+      if (unit >= hi) return;
+    }
     __syncthreads();  // the share has been read
-    unit += w.whole ? 1 : t1 - t0;
   }
 }
 
@@ -485,17 +536,18 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
 // then the first slots of those after it, in their order. One workgroup to a workgroup of the other kernel and a combination; most
 // have nothing to do.
 template <int D, int NC>
-__global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedPool pool, PagedWork w, uint32_t grid) {
+__global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedWork w, uint32_t page_log2, const int32_t* __restrict__ lens,
+                                                                   const int32_t* __restrict__ starts, uint32_t grid) {
   constexpr int kLanes = D / 4, kParts = 256 / kLanes;
   const uint32_t g = blockIdx.x;
   const int combo = blockIdx.y;
   const PagedTail t = reinterpret_cast<const PagedTail*>(w.workspace)[g];
   if (!t.owner) return;
-  const PagedSequence s = paged_sequence<NC>(w, pool, t.seq);
+  const PagedSequence s = paged_sequence<NC>(w, page_log2, lens, starts, t.seq);
   const uint64_t which = (uint64_t)(uint32_t)t.tile * NC + combo;
   if (which >= (uint64_t)s.rows * w.per) return;
   // the workgroup that has the segment's last unit: about (end - 1) groups / units
-  uint32_t last = (uint32_t)((double)(t.end - 1) * t.groups / (double)t.units);
+  uint32_t last = (uint32_t)((uint64_t)(t.end - 1) * t.groups / t.units);
   last = min(last, t.groups - 1);
   while (last + 1 < t.groups && first_unit(t.units, t.groups, last + 1) < t.end) ++last;
   while (first_unit(t.units, t.groups, last) >= t.end) --last;
@@ -541,25 +593,15 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedPool poo
   *reinterpret_cast<uint2*>(w.out + to) = make_uint2(pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv));
 }
 
-// Columns to a combination: as many of the groups as leave room for the combinations that a sequence has on average. (Shares of
-// 16 combinations and the sums of more than 2048 sequences would not fit the 64 KB of LDS of a launch.)
+// Columns to a combination: as many of the groups as leave room for the combinations that a sequence has on average.
 int columns_of(int head_dim, int64_t rows, int64_t seqs, int64_t per) {
   const int64_t combinations = per * ((rows + seqs - 1) / seqs);
   if (head_dim == 128 && combinations <= 4) return 4;
-  return combinations <= 8 || seqs > 2048 ? 2 : 1;
+  return combinations <= 8 ? 2 : 1;
 }
 
 // Tokens up to which a sequence is not split over workgroups.
-bool is_whole(int64_t most_keys) { return most_keys <= 512; }
-
-// Workgroups: no more than there can be units.
-int64_t groups_of(int nc, int64_t rows, int64_t seqs, int64_t per, int64_t kv_heads, int64_t most_keys) {
-  const int64_t tiles = rows * per / nc + (seqs < rows ? seqs : rows);  // at most: of combinations, of all sequences
-  const int64_t units = is_whole(most_keys) ? 1 : ((most_keys + kTile - 1) / kTile + 3) / 4;
-  return tiles >= kMostGroups || tiles * kv_heads >= kMostGroups || units >= kMostGroups || tiles * kv_heads * units >= kMostGroups
-             ? kMostGroups
-             : tiles * kv_heads * units;
-}
+bool is_whole(int64_t most_keys) { return most_keys <= 1024; }
 
 }  // namespace
 
@@ -577,15 +619,35 @@ hipError_t launch_paged_attention(int scale_kind, bool asym, int head_dim, const
   const int64_t most_keys = max_keys > 0 && max_keys < width ? max_keys : width;
   const int gc = columns_of(head_dim, rows, seqs, per), nc = 16 / gc;
   const bool whole = is_whole(most_keys);
-  const int64_t grid = groups_of(nc, rows, seqs, per, pool.kv_heads, most_keys);
-  const PagedWork w = {q, table, lens, starts, positions, out, static_cast<uint8_t*>(workspace), rows, max_pages, (int)seqs, (int)q_heads,
-                       (int)per, scale * 1.4426950408889634f, whole ? 1 : 0};
+  // at most so many tiles of combinations have all sequences together, and so many units
+  const int64_t tiles = (rows * per / nc + (seqs < rows ? seqs : rows)) * pool.kv_heads, tokens = (width + kTile - 1) / kTile;
+  int unit_log2 = 0;
+  while (tiles >= (int64_t(1) << 31) / ((tokens >> unit_log2) + 1)) ++unit_log2;
+  const PagedWork w = {q, out, static_cast<uint8_t*>(workspace), rows, max_pages, (int)seqs, (int)q_heads, (int)per,
+                       scale * 1.4426950408889634f, whole ? 1 : 0, unit_log2};
   const size_t values = 4 * kTile * (size_t)head_dim / 2, shares = 4 * (size_t)nc * head_dim * sizeof(float);
-  const size_t lds = (((size_t)seqs * 8 + 15) & ~(size_t)15) + (values > shares ? values : shares);
+  const int64_t segments = seqs * pool.kv_heads;
+  const bool by_wave = whole && segments >= 512;
+  dim3 grid;
+  size_t lds = values;
+  if (whole) {
+    // tiles of combinations of one sequence: as many as there are on average, at least
+    const int64_t ct = (rows * per + seqs * nc - 1) / (seqs * nc);
+    grid = dim3((unsigned)(by_wave ? (segments + 3) / 4 : segments), (unsigned)(ct < 1024 ? ct : 1024));
+    if (!by_wave && shares > values) lds = shares;
+  } else {
+    const int64_t units = tiles * ((((most_keys + kTile - 1) / kTile) >> unit_log2) / 4 + 1);
+    grid = dim3((unsigned)(units < kMostGroups ? units : kMostGroups));
+    lds = (((size_t)seqs * 4 + 15) & ~(size_t)15) + (values > shares ? values : shares);
+  }
   auto go = [&]<int SK, bool ASYM, int D, int GC>() {
-    hipLaunchKernelGGL((paged_attention_kernel<SK, ASYM, D, GC>), dim3((unsigned)grid), dim3(256), lds, s, pool, w);
+    if (by_wave)
+      hipLaunchKernelGGL((paged_attention_kernel<SK, ASYM, D, GC, 1>), grid, dim3(256), lds, s, pool, w, table, lens, starts, positions);
+    else
+      hipLaunchKernelGGL((paged_attention_kernel<SK, ASYM, D, GC, 4>), grid, dim3(256), lds, s, pool, w, table, lens, starts, positions);
     if (!whole)
-      hipLaunchKernelGGL((paged_attention_join_kernel<D, 16 / GC>), dim3((unsigned)grid, 16 / GC), dim3(256), 0, s, pool, w, (uint32_t)grid);
+      hipLaunchKernelGGL((paged_attention_join_kernel<D, 16 / GC>), dim3(grid.x, 16 / GC), dim3(256), 0, s, w, pool.page_log2, lens, starts,
+                         grid.x);
     return hipGetLastError();
   };
   auto with_format = [&]<int SK, bool ASYM>() {
