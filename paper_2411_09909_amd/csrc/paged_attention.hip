@@ -163,25 +163,23 @@ struct PagedTile {
   static constexpr int kScaleWords = (ASYM ? 8 : 4);      // scales of 16 tokens
   u32x4 k[NK], v[NV];
   u32x4 ks[GS][kScaleWords / 4], vs[GS][kScaleWords / 4];
-  uint32_t bad;  // sub-blocks of 16 tokens whose page is none
 };
 
 // SHARE: waves to a sequence and key head, 4 or 1.
 template <int SCALE_KIND, bool ASYM, int D, int GC, int SHARE>
-__global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void paged_attention_kernel(
+__global__ __launch_bounds__(256, D == 64 || (GC == 4 && SHARE == 4) || (!ASYM && GC >= 2) ? 3 : 2) void paged_attention_kernel(
     PagedPool pool, PagedWork w, const int32_t* __restrict__ table, const int32_t* __restrict__ lens, const int32_t* __restrict__ starts,
     const int32_t* __restrict__ positions) {
   using Tile = PagedTile<SCALE_KIND, ASYM, D, GC>;
   constexpr int GS = Tile::GS, NC = 16 / GC, DT = D / 16;
   constexpr int kValueBytes = kTile * D / 2;  // of a wave's tile of V
   constexpr int kShareFloats = NC * D;
-  extern __shared__ __align__(16) uint8_t lds[];
+  extern __shared__ __align__(64) uint8_t lds[];
   __shared__ float top_of[4][NC], sum_of[4][NC];
 
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = lane & 15, u = lane >> 4, c = r / GC, gc = r % GC;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t* const ends = reinterpret_cast<uint32_t*>(lds);  // split: units up to and with a sequence
-  uint8_t* const region = lds + (w.whole ? 0 : ((size_t)w.seqs * 4 + 15) & ~(size_t)15);
+  uint8_t* const region = lds + (w.whole ? 0 : ((size_t)w.seqs * 4 + 63) & ~(size_t)63);
   uint8_t* const mine = region + wave * kValueBytes;
 
   int b, head;
@@ -192,6 +190,7 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
     b = __builtin_amdgcn_readfirstlane((int)(which / pool.kv_heads)), head = (int)which - b * (int)pool.kv_heads;
     ct = blockIdx.y;
   } else {
+    const int lane = threadIdx.x & 63;
     // ---- the workgroup's range of units. The sums stay at kMostUnits once they reach it, which only rows that sequences share
     // can bring about: then units are missing, but each is one of its sequence's.
     constexpr uint32_t kMostUnits = 0x7FFFFFFF;
@@ -231,6 +230,10 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
   }
 
   for (;;) {
+    // (the lane anew here and below the tiles: what depends on it would otherwise be worked out before and take 50 registers)
+    uint32_t thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));
+    const int lane = thread & 63, r = lane & 15, u = lane >> 4, c = r / GC, gc = r % GC;
     uint32_t t0 = 0, t1, after = 0;  // tiles of tokens; the unit behind the segment's last
     bool complete = true;
     if (SHARE == 4 && !w.whole)
@@ -255,59 +258,65 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
     const int32_t* row_table = table + (int64_t)b * w.max_pages;
     const uint32_t last_entry = (uint32_t)(w.max_pages - 1);
 
-    // ---- requests
+    // ---- requests. A tile's registers take the next tile's data once they have been used: K, its scales and V (which is in LDS by
+    // then) after the scores, V's scales after the weights.
     const int64_t page_stride = (int64_t)pool.kv_heads << pool.page_log2;
-    uint32_t id[4];  // pages of the four sub-blocks of 16 tokens of the tile that is requested next
+    const uint32_t mask = (1u << pool.page_log2) - 1;
+    // pages of the four sub-blocks of 16 tokens of the tile that is requested next (four variables: an array would be indexed)
+    uint32_t id0, id1, id2, id3;
     auto look_up = [&](uint32_t tile) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) id[k] = (uint32_t)row_table[min((tile * kTile + 16 * k) >> pool.page_log2, last_entry)];
+      auto entry = [&](uint32_t k) { return (uint32_t)row_table[min((tile * kTile + 16 * k) >> pool.page_log2, last_entry)]; };
+      id0 = entry(0), id1 = entry(1), id2 = entry(2), id3 = entry(3);
     };
-    auto request = [&](uint32_t tile, Tile& d) {
-      d.bad = 0;
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (id[k] >= pool.pages) d.bad |= 1u << k, id[k] = 0;
-      const uint32_t mask = (1u << pool.page_log2) - 1;
-      auto pick = [&](int k) {  // the id of a sub-block that depends on the lane
-        const uint32_t a = k & 1 ? id[1] : id[0], z = k & 1 ? id[3] : id[2];
-        return k & 2 ? z : a;
-      };
-      auto first_token = [&](uint32_t page, uint32_t token) {  // of the pool, for this head: place of a token
-        return (int64_t)page * page_stride + ((int64_t)head << pool.page_log2) + (token & mask);
-      };
-      // K: tile row r of product t is key 16 (r / 4) + 4 t + r % 4
-      {
-        const int k = r >> 2;
-        const uint32_t token = tile * kTile + 16 * k + (r & 3) + (D == 64 ? 4 * (u >> 1) : 0);
-        const uint8_t* p = pool.k_codes + first_token(pick(k), token) * (D / 2) + 16 * (D == 64 ? (u & 1) : u);
-#pragma unroll
-        for (int t = 0; t < Tile::NK; ++t) d.k[t] = *reinterpret_cast<const u32x4*>(p + t * (D == 64 ? 8 : 4) * (D / 2));
-      }
-      // scales of tokens 16 u .. of group s * GC + gc
+    auto in_pool = [&](uint32_t id) { return id < pool.pages ? id : 0u; };
+    auto pick = [&](int k) {  // of a sub-block that depends on the lane
+      const uint32_t a = k & 1 ? id1 : id0, z = k & 1 ? id3 : id2;
+      return in_pool(k & 2 ? z : a);
+    };
+    auto first_token = [&](uint32_t page, uint32_t token) {  // of the pool, for this head: place of a token
+      return (int64_t)page * page_stride + ((int64_t)head << pool.page_log2) + (token & mask);
+    };
+    // scales of tokens 16 u .. of group st * GC + gc
+    auto request_scales = [&](uint32_t tile, const uint8_t* from, u32x4 (&to)[GS][Tile::kScaleWords / 4]) {
       const uint32_t place = (tile * kTile + 16 * u) & mask;
       const int64_t at = (((int64_t)pick(u) * pool.kv_heads + head) * Tile::kGroups + gc) << pool.page_log2;
-      const int64_t offset = (at + place) * (ASYM ? 2 : 1);
-      auto scales = [&](const uint8_t* from, u32x4 (&to)[GS][Tile::kScaleWords / 4]) {
+      const uint8_t* p = from + (at + place) * (ASYM ? 2 : 1);
 #pragma unroll
-        for (int st = 0; st < GS; ++st)
+      for (int st = 0; st < GS; ++st)
 #pragma unroll
-          for (int i = 0; i < Tile::kScaleWords / 4; ++i)
-            to[st][i] = *reinterpret_cast<const u32x4*>(from + offset + (((int64_t)st * GC) << pool.page_log2) * (ASYM ? 2 : 1) + 16 * i);
-      };
-      scales(pool.k_scales, d.ks);
+        for (int i = 0; i < Tile::kScaleWords / 4; ++i)
+          to[st][i] = *reinterpret_cast<const u32x4*>(p + (((int64_t)st * GC) << pool.page_log2) * (ASYM ? 2 : 1) + 16 * i);
+    };
+    // K: tile row r of product t is key 16 (r / 4) + 4 t + r % 4
+    auto request_keys = [&](uint32_t tile, Tile& d) {
+      const int k = r >> 2;
+      const uint32_t token = tile * kTile + 16 * k + (r & 3) + (D == 64 ? 4 * (u >> 1) : 0);
+      const uint8_t* p = pool.k_codes + first_token(pick(k), token) * (D / 2) + 16 * (D == 64 ? (u & 1) : u);
+#pragma unroll
+      for (int t = 0; t < Tile::NK; ++t) d.k[t] = *reinterpret_cast<const u32x4*>(p + t * (D == 64 ? 8 : 4) * (D / 2));
+      request_scales(tile, pool.k_scales, d.ks);
+    };
+    auto request_values = [&](uint32_t tile, Tile& d) {
 #pragma unroll
       for (int n = 0; n < Tile::NV; ++n) {
         constexpr int kParts = D / 32;  // pieces of 16 bytes in a row
         const uint32_t token = tile * kTile + n * (64 / kParts) + lane / kParts;
-        const uint32_t page = D == 128 ? id[n] : (lane < 32 ? id[2 * n & 3] : id[(2 * n + 1) & 3]);
+        const uint32_t page = in_pool(D == 128 ? (n == 0 ? id0 : n == 1 ? id1 : n == 2 ? id2 : id3) : n == 0 ? (lane < 32 ? id0 : id1) : (lane < 32 ? id2 : id3));
         d.v[n] = *reinterpret_cast<const u32x4*>(pool.v_codes + first_token(page, token) * (D / 2) + 16 * (lane % kParts));
       }
-      scales(pool.v_scales, d.vs);
     };
-    Tile next;
-    uint32_t tile = t0 + (SHARE == 1 ? 0 : wave);
+    auto bad_pages = [&]() {
+      return (id0 >= pool.pages ? 1u : 0u) | (id1 >= pool.pages ? 2u : 0u) | (id2 >= pool.pages ? 4u : 0u) | (id3 >= pool.pages ? 8u : 0u);
+    };
+    Tile d;
+    uint32_t tile = t0 + (SHARE == 1 ? 0 : wave), bad = 0;
     look_up(tile);
-    if (tile < t1) request(tile, next);
+    if (tile < t1) {
+      bad = bad_pages();
+      request_values(tile, d);
+      request_keys(tile, d);
+      request_scales(tile, pool.v_scales, d.vs);
+    }
     look_up(tile + SHARE);
 
     // ---- this lane's combination
@@ -340,24 +349,21 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
     const float sc = w.scale_log2;
 
     for (; tile < stop; tile += SHARE) {
-      const Tile d = next;
+      const bool more = tile + SHARE < stop;
       // V into LDS, piece p of row j at p ^ (some bits of j): rows that 16 lanes read at once lie in different banks
+      // (the LDS of a launch and `mine` begin at multiples of 64 bytes)
 #pragma unroll
       for (int n = 0; n < Tile::NV; ++n) {
         constexpr int kParts = D / 32;
         const int j = n * (64 / kParts) + lane / kParts, part = (lane % kParts) ^ (D == 128 ? (j >> 2) & 3 : (j >> 3) & 1);
         *reinterpret_cast<u32x4*>(mine + j * (D / 2) + 16 * part) = d.v[n];
       }
-      if (tile + SHARE < stop) {
-        request(tile + SHARE, next);
-        look_up(tile + 2 * SHARE);
-      }
 
       // ---- scores
       float x[16];
       const int first = (int)tile * kTile;
-      const int count = (d.bad >> u) & 1 ? 0 : max(0, min(limit - first - 16 * u, 16));
-      const bool all = first + kTile <= least && d.bad == 0;
+      const int count = (bad >> u) & 1 ? 0 : max(0, min(limit - first - 16 * u, 16));
+      const bool all = first + kTile <= least && bad == 0;
       uint32_t kw[4 * Tile::NK];
 #pragma unroll
       for (int n = 0; n < Tile::NK; ++n) {
@@ -396,11 +402,28 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
           }
         }
       }
+      // (the scores are there before K's registers are asked for again: otherwise the scaling is moved behind the branch, and both the
+      // products and the old scales are kept across it; the same with V's scales below)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(x[i]));
+      if (more) {
+        request_keys(tile + SHARE, d);
+        request_values(tile + SHARE, d);
+      }
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[i] = columns_sum<GC>(x[i]);
       if (!all) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = i < count ? x[i] : -INFINITY;
+        // scales of V that belong to no token seen become zeros: they may be infinite, and weights of 0 would be NaN
+#pragma unroll
+        for (int st = 0; st < GS; ++st)
+#pragma unroll
+          for (int i = 0; i < Tile::kScaleWords; ++i) {
+            constexpr int kTokens = ASYM ? 2 : 4;  // of a word
+            const int seen = max(0, min(count - kTokens * i, kTokens));
+            d.vs[st][i >> 2][i & 3] &= seen == kTokens ? ~0u : (1u << (32 / kTokens * seen)) - 1;
+          }
       }
 
       // ---- running maximum and sum
@@ -419,7 +442,10 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
         for (int i = 0; i < DT; ++i) o[i] *= alpha;
       }
 
-      // ---- values
+      // ---- values. Token 16 u + r's row, its piece 0; piece p is 16 p bytes away in the bits of its place (again for every tile: one
+      // register instead of one to a piece)
+      uint32_t row_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)mine + (16 * u + r) * (D / 2) + 16 * (D == 128 ? (r >> 2) & 3 : (r >> 3) & 1);
+      asm volatile("" : "+v"(row_at));
 #pragma unroll
       for (int st = 0; st < GS; ++st) {
         uint32_t wp[8], wn[8];  // weights of this lane's 16 keys, pairs
@@ -434,12 +460,18 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
             const f32x2 pair = i & 1 ? two_scales<SCALE_KIND, true>(word) : two_scales<SCALE_KIND, false>(word);
             s0 = f32x2{pair[0], pair[0]}, s1 = f32x2{pair[1], pair[1]};
           }
-          if (!all) {  // (what lies behind the last token may be infinite)
-            if (2 * i >= count) s0 = f32x2{0, 0};
-            if (2 * i + 1 >= count) s1 = f32x2{0, 0};
-          }
           wp[i] = pack_bf16(x[2 * i] * s0[0], x[2 * i + 1] * s1[0]);
           if constexpr (ASYM) wn[i] = pack_bf16(x[2 * i] * s0[1], x[2 * i + 1] * s1[1]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          asm volatile("" : "+v"(wp[i]));
+          if constexpr (ASYM) asm volatile("" : "+v"(wn[i]));
+        }
+        if (st == GS - 1 && more) {
+          request_scales(tile + SHARE, pool.v_scales, d.vs);
+          bad = bad_pages();
+          look_up(tile + 2 * SHARE);
         }
         const bf16x8 p0 = __builtin_bit_cast(bf16x8, (u32x4{wp[0], wp[1], wp[2], wp[3]})), p1 = __builtin_bit_cast(bf16x8, (u32x4{wp[4], wp[5], wp[6], wp[7]}));
         bf16x8 n0, n1;
@@ -447,9 +479,8 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
           n0 = __builtin_bit_cast(bf16x8, (u32x4{wn[0], wn[1], wn[2], wn[3]})), n1 = __builtin_bit_cast(bf16x8, (u32x4{wn[4], wn[5], wn[6], wn[7]}));
 #pragma unroll
         for (int dt = 2 * GC * st; dt < 2 * GC * (st + 1); ++dt) {
-          const int j = 16 * u + r, part = (dt >> 1) ^ (D == 128 ? (j >> 2) & 3 : (j >> 3) & 1);
           typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
-          const i32x2 codes = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2*)(mine + j * (D / 2) + 16 * part + 8 * (dt & 1)));
+          const i32x2 codes = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2*)(uintptr_t)((row_at ^ (16 * (dt >> 1))) + 8 * (dt & 1)));
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const u32x4 e = elements((uint32_t)codes[h]);
@@ -465,13 +496,22 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
     }
 
     l = quarters_sum(l);
+    thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));
+    const int to_u = (int)(thread & 63) >> 4, to_c = (int)(thread & 15) / GC, to_gc = (int)(thread & 15) % GC;
+    // where a combination's result goes
+    auto destination = [&](uint64_t which) {
+      const uint32_t i = (uint32_t)(which / (uint32_t)w.per), h = (uint32_t)(which % (uint32_t)w.per);
+      return w.out + ((s.first + i) * w.q_heads + (int64_t)head * w.per + h) * D;
+    };
     if constexpr (SHARE == 1) {
       const float inv = l > 0.f ? 1.0f / l : 0.f;
-      if (asked) {
-        uint16_t* to = w.out + (row * w.q_heads + (int64_t)head * w.per + head_of) * D + 4 * u;
+      const uint64_t which = (uint64_t)ct * NC + to_c;
+      if (which < (uint64_t)s.rows * w.per) {
+        uint16_t* to = destination(which) + 4 * to_u;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
-          if ((dt >> 1) % GC == gc) {
+          if ((dt >> 1) % GC == to_gc) {
             const f32x4 v = o[dt] * inv;
             *reinterpret_cast<uint2*>(to + dt * 16) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
           }
@@ -481,20 +521,20 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
     }
 
     // ---- the four waves' shares, each against its own maximum, become one
-    if (u == 0 && gc == 0) top_of[wave][c] = m, sum_of[wave][c] = l;
+    if (to_u == 0 && to_gc == 0) top_of[wave][to_c] = m, sum_of[wave][to_c] = l;
     __syncthreads();  // (and all waves have read their V)
-    const float top = fmaxf(fmaxf(top_of[0][c], top_of[1][c]), fmaxf(top_of[2][c], top_of[3][c]));
+    const float top = fmaxf(fmaxf(top_of[0][to_c], top_of[1][to_c]), fmaxf(top_of[2][to_c], top_of[3][to_c]));
     const float factor = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * sc);
     float* share = reinterpret_cast<float*>(region);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
-      if ((dt >> 1) % GC == gc) *reinterpret_cast<f32x4*>(share + wave * kShareFloats + c * D + dt * 16 + 4 * u) = o[dt] * factor;
+      if ((dt >> 1) % GC == to_gc) *reinterpret_cast<f32x4*>(share + wave * kShareFloats + to_c * D + dt * 16 + 4 * to_u) = o[dt] * factor;
     __syncthreads();
     float* part = nullptr;
     if (!complete)  // slot 0: begun by another workgroup, 1: begun here
       part = reinterpret_cast<float*>(w.workspace + (((size_t)gridDim.x * sizeof(PagedTail) + 255) & ~(size_t)255)) +
              (2 * (size_t)blockIdx.x + (t0 == 0 ? 1 : 0)) * kPartFloats<NC, D>;
-    for (int i = threadIdx.x; i < kShareFloats / 2; i += 256) {
+    for (int i = (int)thread; i < kShareFloats / 2; i += 256) {
       const int combo = 2 * i / D, dim = 2 * i % D;
       float2 v = *reinterpret_cast<const float2*>(share + 2 * i);
 #pragma unroll
@@ -511,8 +551,7 @@ __global__ __launch_bounds__(256, ASYM && D == 128 && GC == 1 ? 1 : 2) void page
         const uint64_t which = (uint64_t)ct * NC + combo;
         if (which < (uint64_t)s.rows * w.per) {
           const float inv = total > 0.f ? 1.0f / total : 0.f;
-          const int64_t to = ((s.first + (int64_t)(which / (uint32_t)w.per)) * w.q_heads + (int64_t)head * w.per + (int64_t)(which % (uint32_t)w.per)) * D + dim;
-          *reinterpret_cast<uint32_t*>(w.out + to) = pack_bf16(v.x * inv, v.y * inv);
+          *reinterpret_cast<uint32_t*>(destination(which) + dim) = pack_bf16(v.x * inv, v.y * inv);
         }
       } else {
         *reinterpret_cast<float2*>(part + 2 * i) = v;
@@ -638,7 +677,7 @@ hipError_t launch_paged_attention(int scale_kind, bool asym, int head_dim, const
   } else {
     const int64_t units = tiles * ((((most_keys + kTile - 1) / kTile) >> unit_log2) / 4 + 1);
     grid = dim3((unsigned)(units < kMostGroups ? units : kMostGroups));
-    lds = (((size_t)seqs * 4 + 15) & ~(size_t)15) + (values > shares ? values : shares);
+    lds = (((size_t)seqs * 4 + 63) & ~(size_t)63) + (values > shares ? values : shares);
   }
   auto go = [&]<int SK, bool ASYM, int D, int GC>() {
     if (by_wave)
