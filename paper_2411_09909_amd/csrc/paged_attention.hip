@@ -102,12 +102,17 @@ __device__ __forceinline__ float quarters_sum(float v) {
   return u2f(b[0]) + u2f(b[1]);
 }
 
-// sum over the GC neighbouring columns of a combination (1, 2 or 4 lanes)
-template <int GC>
-__device__ __forceinline__ float columns_sum(float v) {
-  if constexpr (GC >= 2) v += u2f((uint32_t)__builtin_amdgcn_mov_dpp((int)f2u(v), 0xB1, 0xF, 0xF, true));
-  if constexpr (GC >= 4) v += u2f((uint32_t)__builtin_amdgcn_mov_dpp((int)f2u(v), 0x4E, 0xF, 0xF, true));
-  return v;
+// A lane's neighbours among the GC columns of a combination (GC 2 or 4): lane ^ 1, lane ^ 2.
+template <int X>
+__device__ __forceinline__ float neighbour(float v) {
+  return u2f((uint32_t)__builtin_amdgcn_mov_dpp((int)f2u(v), X == 1 ? 0xB1 : 0x4E, 0xF, 0xF, true));
+}
+// the value of column G of the combination, in all its columns
+template <int GC, int G>
+__device__ __forceinline__ float of_column(float v) {
+  if constexpr (GC == 1) return v;
+  constexpr int kPerm = GC == 4 ? G * 0x55 : G + (G << 2) + ((2 + G) << 4) + ((2 + G) << 6);
+  return u2f((uint32_t)__builtin_amdgcn_mov_dpp((int)f2u(v), kPerm, 0xF, 0xF, true));
 }
 
 // Two scales (bytes 2 HALF and 2 HALF + 1 of a word) as floats.
@@ -159,6 +164,7 @@ __device__ __forceinline__ u32x4 negative(u32x4 e) {
 template <int SCALE_KIND, bool ASYM, int D, int GC>
 struct PagedTile {
   static constexpr int kGroups = D / 32, GS = kGroups / GC;
+  static constexpr bool kAsLoaded = D == 128 && GC == 4;  // a lane has the four words of the group of its quarter, and the products take one each
   static constexpr int NK = D / 32, NV = D / 32;          // loads of 16 bytes: codes of K, of V
   static constexpr int kScaleWords = (ASYM ? 8 : 4);      // scales of 16 tokens
   u32x4 k[NK], v[NV];
@@ -332,13 +338,15 @@ __global__ __launch_bounds__(256, D == 64 || (GC == 4 && SHARE == 4) || (!ASYM &
     least = __builtin_amdgcn_readfirstlane(least), most = __builtin_amdgcn_readfirstlane(most);
     const uint32_t stop = min(t1, (uint32_t)(most + kTile - 1) / kTile);
 
-    // ---- the query: dimensions 32 j + 8 u .. of group j, zeros where the column is not the group's
+    // ---- the query: dimensions 32 j + 8 u .. of group j, zeros where the column is not the group's; where the keys' words stay as
+    // they are loaded (all groups in the columns), dimensions 32 u + 8 j .. of group u
     u32x4 q[Tile::kGroups];
 #pragma unroll
     for (int j = 0; j < Tile::kGroups; ++j) {
       q[j] = u32x4{0, 0, 0, 0};
-      if (asked && j % GC == gc)
-        q[j] = *reinterpret_cast<const u32x4*>(w.q + (row * w.q_heads + (int64_t)head * w.per + head_of) * D + 32 * j + 8 * u);
+      if (asked && (Tile::kAsLoaded ? u : j % GC) == gc)
+        q[j] = *reinterpret_cast<const u32x4*>(w.q + (row * w.q_heads + (int64_t)head * w.per + head_of) * D +
+                                               (Tile::kAsLoaded ? 32 * u + 8 * j : 32 * j + 8 * u));
     }
 
     // ---- the tiles
@@ -367,6 +375,10 @@ __global__ __launch_bounds__(256, D == 64 || (GC == 4 && SHARE == 4) || (!ASYM &
       uint32_t kw[4 * Tile::NK];
 #pragma unroll
       for (int n = 0; n < Tile::NK; ++n) {
+        if constexpr (Tile::kAsLoaded) {
+          for (int j = 0; j < 4; ++j) kw[4 * n + j] = d.k[n][j];
+          continue;
+        }
         // a lane has the four words of one group; it is to have word u of each of the four: the quarters' 4 x 4 words transposed
         const auto a = __builtin_amdgcn_permlane32_swap(d.k[n][0], d.k[n][2], false, false);
         const auto z = __builtin_amdgcn_permlane32_swap(d.k[n][1], d.k[n][3], false, false);
@@ -410,11 +422,28 @@ __global__ __launch_bounds__(256, D == 64 || (GC == 4 && SHARE == 4) || (!ASYM &
         request_keys(tile + SHARE, d);
         request_values(tile + SHARE, d);
       }
+      // The columns' sums, each column keeping those of its share of the lane's 16 keys: key GC k + gc as y[k]. The rest of the softmax
+      // is done for those alone.
+      constexpr int kMine = 16 / GC;
+      float y[kMine];
+      if constexpr (GC == 4) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = columns_sum<GC>(x[i]);
+        for (int k = 0; k < 4; ++k) {
+          const bool odd = gc & 1, high = gc & 2;
+          const float a = (odd ? x[4 * k + 1] : x[4 * k]) + neighbour<1>(odd ? x[4 * k] : x[4 * k + 1]);
+          const float z = (odd ? x[4 * k + 3] : x[4 * k + 2]) + neighbour<1>(odd ? x[4 * k + 2] : x[4 * k + 3]);
+          y[k] = (high ? z : a) + neighbour<2>(high ? a : z);
+        }
+      } else if constexpr (GC == 2) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) y[k] = (gc ? x[2 * k + 1] : x[2 * k]) + neighbour<1>(gc ? x[2 * k] : x[2 * k + 1]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) y[k] = x[k];
+      }
       if (!all) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = i < count ? x[i] : -INFINITY;
+        for (int k = 0; k < kMine; ++k) y[k] = GC * k + gc < count ? y[k] : -INFINITY;
         // scales of V that belong to no token seen become zeros: they may be infinite, and weights of 0 would be NaN
 #pragma unroll
         for (int st = 0; st < GS; ++st)
@@ -427,15 +456,17 @@ __global__ __launch_bounds__(256, D == 64 || (GC == 4 && SHARE == 4) || (!ASYM &
       }
 
       // ---- running maximum and sum
-      float top = x[0];
+      float top = y[0];
 #pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+      for (int k = 1; k < kMine; ++k) top = fmaxf(top, y[k]);
+      if constexpr (GC >= 2) top = fmaxf(top, neighbour<1>(top));
+      if constexpr (GC >= 4) top = fmaxf(top, neighbour<2>(top));
       top = fmaxf(m, quarters_max(top));
       const float to = top == -INFINITY ? 0.f : top, alpha = __builtin_amdgcn_exp2f((m - to) * sc), shift = to * sc;
       m = top;
       float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], sc, -shift)), sum += x[i];
+      for (int k = 0; k < kMine; ++k) y[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(y[k], sc, -shift)), sum += y[k];
       l = __builtin_fmaf(l, alpha, sum);
       if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
 #pragma unroll
@@ -460,8 +491,12 @@ __global__ __launch_bounds__(256, D == 64 || (GC == 4 && SHARE == 4) || (!ASYM &
             const f32x2 pair = i & 1 ? two_scales<SCALE_KIND, true>(word) : two_scales<SCALE_KIND, false>(word);
             s0 = f32x2{pair[0], pair[0]}, s1 = f32x2{pair[1], pair[1]};
           }
-          wp[i] = pack_bf16(x[2 * i] * s0[0], x[2 * i + 1] * s1[0]);
-          if constexpr (ASYM) wn[i] = pack_bf16(x[2 * i] * s0[1], x[2 * i + 1] * s1[1]);
+          // keys 2 i and 2 i + 1: each from the column that has it
+          const float v = y[2 * i / GC], z = y[(2 * i + 1) / GC];
+          const float a = GC == 4 && (i & 1) ? of_column<GC, GC == 4 ? 2 : 0>(v) : of_column<GC, 0>(v);
+          const float e = GC == 4 && (i & 1) ? of_column<GC, GC == 4 ? 3 : 0>(z) : of_column<GC, GC >= 2 ? 1 : 0>(z);
+          wp[i] = pack_bf16(a * s0[0], e * s1[0]);
+          if constexpr (ASYM) wn[i] = pack_bf16(a * s0[1], e * s1[1]);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -496,6 +531,8 @@ __global__ __launch_bounds__(256, D == 64 || (GC == 4 && SHARE == 4) || (!ASYM &
     }
 
     l = quarters_sum(l);
+    if constexpr (GC >= 2) l += neighbour<1>(l);
+    if constexpr (GC >= 4) l += neighbour<2>(l);
     thread = threadIdx.x;
     asm volatile("" : "+v"(thread));
     const int to_u = (int)(thread & 63) >> 4, to_c = (int)(thread & 15) / GC, to_gc = (int)(thread & 15) % GC;
