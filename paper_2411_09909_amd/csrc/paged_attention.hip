@@ -41,7 +41,10 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short i16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTile = 64;        // tokens of a unit
-constexpr int kMostGroups = 1024;  // workgroups
+constexpr int kMostWorkers = 3072;
+// A sequence, key head and tile of combinations takes as long as this many tiles before its first one is in: the chain from the lengths
+// over the table to the keys, and the joining of the waves.
+constexpr uint32_t kStart = 12;
 
 // What one launch reads, beside the arrays of the sequences.
 struct PagedWork {
@@ -54,16 +57,16 @@ struct PagedWork {
   int whole, unit_log2;    // tiles of 64 tokens to a unit
 };
 
-// What a workgroup leaves behind for the joining kernel, at the front of the workspace.
+// What a worker (a workgroup or a wave) leaves behind for the joining kernel, at the front of the workspace.
 struct PagedTail {
-  uint32_t units, end;    // all units; one past the last of the sequence, key head and tile that this workgroup began and did not end
-  uint32_t groups, owner;  // workgroups among which the units are divided; 1: it began such a one
+  uint32_t units, end;    // all units; one past the last of the sequence, key head and tile that this worker began and did not end
+  uint32_t groups, owner;  // workers among which the units are divided; 1: it began such a one
   int32_t seq, head, tile, pad;
 };
 
-// units of a workgroup: [first_unit(g), first_unit(g + 1))
+// units of a worker: [first_unit(g), first_unit(g + 1))
 __device__ __forceinline__ uint32_t first_unit(uint32_t units, uint32_t groups, uint32_t g) {
-  return units / groups * g + (units % groups) * g / groups;  // (groups <= 1024)
+  return units / groups * g + (units % groups) * g / groups;  // (groups <= 3072)
 }
 
 template <int NC, int D>
@@ -173,7 +176,7 @@ struct PagedTile {
 
 // SHARE: waves to a sequence and key head, 4 or 1.
 template <int SCALE_KIND, bool ASYM, int D, int GC, int SHARE>
-__global__ __launch_bounds__(256, D == 64 || (GC == 4 && SHARE == 4) || (!ASYM && GC >= 2) ? 3 : 2) void paged_attention_kernel(
+__global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 : 2) void paged_attention_kernel(
     PagedPool pool, PagedWork w, const int32_t* __restrict__ table, const int32_t* __restrict__ lens, const int32_t* __restrict__ starts,
     const int32_t* __restrict__ positions) {
   using Tile = PagedTile<SCALE_KIND, ASYM, D, GC>;
@@ -190,14 +193,16 @@ __global__ __launch_bounds__(256, D == 64 || (GC == 4 && SHARE == 4) || (!ASYM &
 
   int b, head;
   uint32_t ct = 0, unit = 0, hi = 0;
-  if (SHARE == 1 || w.whole) {
-    const uint32_t which = SHARE == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
-    if (which >= (uint32_t)w.seqs * pool.kv_heads) return;  // (SHARE == 1: the wave; nobody waits for it)
-    b = __builtin_amdgcn_readfirstlane((int)(which / pool.kv_heads)), head = (int)which - b * (int)pool.kv_heads;
+  const uint32_t worker = SHARE == 1 ? blockIdx.x * 4 + wave : blockIdx.x, workers = SHARE == 1 ? gridDim.x * 4 : gridDim.x;
+  // units of a sequence, key head and tile of combinations
+  auto units_of = [&](uint32_t NT) { return kStart + ((NT + (1u << w.unit_log2) - 1) >> w.unit_log2); };
+  if (w.whole) {
+    if (worker >= (uint32_t)w.seqs * pool.kv_heads) return;  // (SHARE == 1: the wave; nobody waits for it)
+    b = __builtin_amdgcn_readfirstlane((int)(worker / pool.kv_heads)), head = (int)worker - b * (int)pool.kv_heads;
     ct = blockIdx.y;
   } else {
     const int lane = threadIdx.x & 63;
-    // ---- the workgroup's range of units. The sums stay at kMostUnits once they reach it, which only rows that sequences share
+    // ---- the worker's range of units. The sums stay at kMostUnits once they reach it, which only rows that sequences share
     // can bring about: then units are missing, but each is one of its sequence's.
     constexpr uint32_t kMostUnits = 0x7FFFFFFF;
     __shared__ uint32_t edge[4];
@@ -205,8 +210,8 @@ __global__ __launch_bounds__(256, D == 64 || (GC == 4 && SHARE == 4) || (!ASYM &
     uint32_t sum = 0;
     for (int i = b0; i < b1; ++i) {
       const PagedSequence s = paged_sequence<NC>(w, pool.page_log2, lens, starts, i);
-      const uint64_t mine = min((uint64_t)s.CT * ((s.NT + (1u << w.unit_log2) - 1) >> w.unit_log2), (uint64_t)kMostUnits) * pool.kv_heads;
-      ends[i] = sum = (uint32_t)min(sum + mine, (uint64_t)kMostUnits);
+      const uint64_t own = min((uint64_t)s.CT * units_of(s.NT), (uint64_t)kMostUnits) * pool.kv_heads;
+      ends[i] = sum = (uint32_t)min(sum + own, (uint64_t)kMostUnits);
     }
     uint32_t upto = sum;
 #pragma unroll
@@ -222,11 +227,11 @@ __global__ __launch_bounds__(256, D == 64 || (GC == 4 && SHARE == 4) || (!ASYM &
     for (int i = b0; i < b1; ++i) ends[i] = min(ends[i] + before, kMostUnits);
     __syncthreads();
     const uint32_t units = __builtin_amdgcn_readfirstlane(ends[w.seqs - 1]);
-    // a tile to each wave at least
-    const uint32_t groups = max(1u, min((uint32_t)gridDim.x, w.unit_log2 ? units : (units + 3) / 4)), g = blockIdx.x;
-    if (threadIdx.x == 0) reinterpret_cast<PagedTail*>(w.workspace)[g] = PagedTail{units, 0, groups, 0, 0, 0, 0, 0};
-    if (g >= groups || units == 0) return;
-    unit = first_unit(units, groups, g), hi = first_unit(units, groups, g + 1);
+    // four units at least
+    const uint32_t groups = max(1u, min(workers, w.unit_log2 ? units : (units + 3) / 4));
+    if ((threadIdx.x & (SHARE == 1 ? 63 : 255)) == 0) reinterpret_cast<PagedTail*>(w.workspace)[worker] = PagedTail{units, 0, groups, 0, 0, 0, 0, 0};
+    if (worker >= groups || units == 0) return;
+    unit = first_unit(units, groups, worker), hi = first_unit(units, groups, worker + 1);
     // the first sequence whose units end behind the range's first: its 64th of the sequences, then in there
     const int part = (w.seqs + 63) >> 6;
     const int chunk = (int)__popcll(__builtin_amdgcn_ballot_w64(ends[min((lane + 1) * part, w.seqs) - 1] <= unit));
@@ -242,22 +247,25 @@ __global__ __launch_bounds__(256, D == 64 || (GC == 4 && SHARE == 4) || (!ASYM &
     const int lane = thread & 63, r = lane & 15, u = lane >> 4, c = r / GC, gc = r % GC;
     uint32_t t0 = 0, t1, after = 0;  // tiles of tokens; the unit behind the segment's last
     bool complete = true;
-    if (SHARE == 4 && !w.whole)
+    if (!w.whole) {
+      if (unit >= hi) return;
       while (__builtin_amdgcn_readfirstlane(ends[b]) <= unit) ++b;
+    }
     const PagedSequence s = paged_sequence<NC>(w, pool.page_log2, lens, starts, b);
-    if (SHARE == 1 || w.whole) {
+    if (w.whole) {
       if (ct >= s.CT) return;
       t1 = s.NT;
     } else {
       const uint32_t base = b ? __builtin_amdgcn_readfirstlane(ends[b - 1]) : 0u;
-      const uint32_t per_segment = (s.NT + (1u << w.unit_log2) - 1) >> w.unit_log2;
+      const uint32_t per_segment = units_of(s.NT);
       const uint32_t seg = (unit - base) / per_segment, first = (unit - base) - seg * per_segment;
       head = (int)(seg / s.CT), ct = seg - (uint32_t)head * s.CT;
       after = base + (seg + 1) * per_segment;
       const uint32_t end = min(per_segment, first + (hi - unit));
-      t0 = first << w.unit_log2, t1 = min(s.NT, end << w.unit_log2);
-      complete = first == 0 && end == per_segment;
       unit += end - first;
+      if (end <= kStart) continue;  // its start alone: what comes after is the next worker's
+      t0 = first > kStart ? (first - kStart) << w.unit_log2 : 0u, t1 = min(s.NT, (end - kStart) << w.unit_log2);
+      complete = t0 == 0 && end == per_segment;
     }
     t0 = __builtin_amdgcn_readfirstlane(t0), t1 = __builtin_amdgcn_readfirstlane(t1);
     ct = __builtin_amdgcn_readfirstlane(ct), head = __builtin_amdgcn_readfirstlane(head);
@@ -541,19 +549,37 @@ __global__ __launch_bounds__(256, D == 64 || (GC == 4 && SHARE == 4) || (!ASYM &
       const uint32_t i = (uint32_t)(which / (uint32_t)w.per), h = (uint32_t)(which % (uint32_t)w.per);
       return w.out + ((s.first + i) * w.q_heads + (int64_t)head * w.per + h) * D;
     };
+    // where a part of one goes: slot 0, begun by another worker, or 1, begun here
+    auto part_of = [&]() {
+      return reinterpret_cast<float*>(w.workspace + (((size_t)workers * sizeof(PagedTail) + 255) & ~(size_t)255)) +
+             (2 * (size_t)worker + (t0 == 0 ? 1 : 0)) * kPartFloats<NC, D>;
+    };
+    auto leave_tail = [&]() {
+      PagedTail* tail = reinterpret_cast<PagedTail*>(w.workspace) + worker;
+      tail->end = after, tail->owner = 1, tail->seq = b, tail->head = head, tail->tile = (int32_t)ct;
+    };
     if constexpr (SHARE == 1) {
-      const float inv = l > 0.f ? 1.0f / l : 0.f;
-      const uint64_t which = (uint64_t)ct * NC + to_c;
-      if (which < (uint64_t)s.rows * w.per) {
-        uint16_t* to = destination(which) + 4 * to_u;
+      if (complete) {
+        const float inv = l > 0.f ? 1.0f / l : 0.f;
+        const uint64_t which = (uint64_t)ct * NC + to_c;
+        if (which < (uint64_t)s.rows * w.per) {
+          uint16_t* to = destination(which) + 4 * to_u;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+            if ((dt >> 1) % GC == to_gc) {
+              const f32x4 v = o[dt] * inv;
+              *reinterpret_cast<uint2*>(to + dt * 16) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+            }
+        }
+      } else {
+        float* part = part_of();
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
-          if ((dt >> 1) % GC == to_gc) {
-            const f32x4 v = o[dt] * inv;
-            *reinterpret_cast<uint2*>(to + dt * 16) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-          }
+          if ((dt >> 1) % GC == to_gc) *reinterpret_cast<f32x4*>(part + to_c * D + dt * 16 + 4 * to_u) = o[dt];
+        if (to_u == 0 && to_gc == 0) part[NC * D + to_c] = m * sc, part[NC * D + NC + to_c] = l;
+        if (t0 == 0 && (thread & 63) == 0) leave_tail();
       }
-      ct += gridDim.y;
+      if (w.whole) ct += gridDim.y;
       continue;
     }
 
@@ -567,10 +593,7 @@ __global__ __launch_bounds__(256, D == 64 || (GC == 4 && SHARE == 4) || (!ASYM &
     for (int dt = 0; dt < DT; ++dt)
       if ((dt >> 1) % GC == to_gc) *reinterpret_cast<f32x4*>(share + wave * kShareFloats + to_c * D + dt * 16 + 4 * to_u) = o[dt] * factor;
     __syncthreads();
-    float* part = nullptr;
-    if (!complete)  // slot 0: begun by another workgroup, 1: begun here
-      part = reinterpret_cast<float*>(w.workspace + (((size_t)gridDim.x * sizeof(PagedTail) + 255) & ~(size_t)255)) +
-             (2 * (size_t)blockIdx.x + (t0 == 0 ? 1 : 0)) * kPartFloats<NC, D>;
+    float* part = complete ? nullptr : part_of();
     for (int i = (int)thread; i < kShareFloats / 2; i += 256) {
       const int combo = 2 * i / D, dim = 2 * i % D;
       float2 v = *reinterpret_cast<const float2*>(share + 2 * i);
@@ -595,78 +618,82 @@ __global__ __launch_bounds__(256, D == 64 || (GC == 4 && SHARE == 4) || (!ASYM &
         if (dim == 0) part[NC * D + combo] = best * sc, part[NC * D + NC + combo] = total;
       }
     }
-    if (w.whole) {
+    if (w.whole)
       ct += gridDim.y;
-    } else {
-      if (!complete && t0 == 0 && threadIdx.x == 0) {
-        PagedTail* tail = reinterpret_cast<PagedTail*>(w.workspace) + blockIdx.x;
-        tail->end = after, tail->owner = 1, tail->seq = b, tail->head = head, tail->tile = (int32_t)ct;
-      }
-      if (unit >= hi) return;
-    }
+    else if (!complete && t0 == 0 && threadIdx.x == 0)
+      leave_tail();
     __syncthreads();  // the share has been read
   }
 }
 
-// Adds up the partial results of one sequence, key head and tile of combinations: the second slot of the workgroup that began it,
-// then the first slots of those after it, in their order. One workgroup to a workgroup of the other kernel and a combination; most
-// have nothing to do.
+// Adds up the partial results of one sequence, key head and tile of combinations: the second slot of the worker that began it, then
+// the first slots of those after it, in their order. One workgroup to a worker of the other kernel; most have nothing to do. A part's floats
+// are shared out over `kLanes` threads, the parts over the rest, eight requests of each under way at once.
 template <int D, int NC>
-__global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedWork w, uint32_t page_log2, const int32_t* __restrict__ lens,
-                                                                   const int32_t* __restrict__ starts, uint32_t grid) {
-  constexpr int kLanes = D / 4, kParts = 256 / kLanes;
+__global__ __launch_bounds__(512) void paged_attention_join_kernel(PagedWork w, uint32_t page_log2, const int32_t* __restrict__ lens,
+                                                                   const int32_t* __restrict__ starts, uint32_t workers) {
+  constexpr int kLanes = NC * D / 4 < 512 ? NC * D / 4 : 512, kSets = 512 / kLanes, kTurns = NC * D / 4 / kLanes;
   const uint32_t g = blockIdx.x;
-  const int combo = blockIdx.y;
   const PagedTail t = reinterpret_cast<const PagedTail*>(w.workspace)[g];
   if (!t.owner) return;
   const PagedSequence s = paged_sequence<NC>(w, page_log2, lens, starts, t.seq);
-  const uint64_t which = (uint64_t)(uint32_t)t.tile * NC + combo;
-  if (which >= (uint64_t)s.rows * w.per) return;
-  // the workgroup that has the segment's last unit: about (end - 1) groups / units
+  // the worker that has the segment's last unit: about (end - 1) groups / units
   uint32_t last = (uint32_t)((uint64_t)(t.end - 1) * t.groups / t.units);
   last = min(last, t.groups - 1);
   while (last + 1 < t.groups && first_unit(t.units, t.groups, last + 1) < t.end) ++last;
   while (first_unit(t.units, t.groups, last) >= t.end) --last;
   const uint32_t count = last - g + 1;
-  const float* parts = reinterpret_cast<const float*>(w.workspace + (((size_t)grid * sizeof(PagedTail) + 255) & ~(size_t)255));
+  const float* parts = reinterpret_cast<const float*>(w.workspace + (((size_t)workers * sizeof(PagedTail) + 255) & ~(size_t)255));
   auto part = [&](uint32_t i) { return parts + (2 * (size_t)(g + i) + (i == 0 ? 1 : 0)) * kPartFloats<NC, D>; };
-  __shared__ float tops[kMostGroups], red[4];
-  __shared__ float4 sums[kParts][kLanes];
-  __shared__ float totals[kParts];
+  __shared__ float tops[8][NC];
+  __shared__ float4 sums[kSets][kLanes];
+  __shared__ float totals[kSets][kLanes];
+  // the combinations' largest: thread (part, combination)
+  constexpr int kEach = 512 / NC;
   float top = -INFINITY;
-  for (uint32_t i = threadIdx.x; i < count; i += 256) {
-    const float v = part(i)[NC * D + combo];
-    tops[i] = v;
-    top = fmaxf(top, v);
-  }
+  for (uint32_t i = threadIdx.x / NC; i < count; i += kEach) top = fmaxf(top, part(i)[NC * D + threadIdx.x % NC]);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
+  for (int o = NC; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  if ((threadIdx.x & 63) < NC) tops[threadIdx.x >> 6][threadIdx.x & 63] = top;
   __syncthreads();
-  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  const int mine = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
-  float4 sum = make_float4(0, 0, 0, 0);
-  float total = 0.f;
-  for (uint32_t i = mine; i < count; i += kParts) {
-    const float f = tops[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(tops[i] - top);
-    const float* p = part(i);
-    const float4 v = *reinterpret_cast<const float4*>(p + combo * D + 4 * lane);
-    sum.x += v.x * f, sum.y += v.y * f, sum.z += v.z * f, sum.w += v.w * f;
-    total += p[NC * D + NC + combo] * f;
-  }
-  sums[mine][lane] = sum;
-  if (lane == 0) totals[mine] = total;
-  __syncthreads();
-  if (mine != 0) return;
+  const int set = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
 #pragma unroll
-  for (int k = 1; k < kParts; ++k) {
-    const float4 v = sums[k][lane];
-    sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
-    total += totals[k];
+  for (int turn = 0; turn < kTurns; ++turn) {
+    const int item = turn * kLanes + lane, combo = item / (D / 4), dim = 4 * (item % (D / 4));
+    float best = tops[0][combo];
+#pragma unroll
+    for (int k = 1; k < 8; ++k) best = fmaxf(best, tops[k][combo]);
+    float4 sum = make_float4(0, 0, 0, 0);
+    float total = 0.f;
+    for (uint32_t i0 = set; i0 < count; i0 += 8 * kSets) {
+      float4 v[8];
+      float m[8], l[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float* p = part(min(i0 + k * kSets, count - 1));
+        v[k] = *reinterpret_cast<const float4*>(p + 4 * item), m[k] = p[NC * D + combo], l[k] = p[NC * D + NC + combo];
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float f = i0 + k * kSets >= count || m[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[k] - best);
+        sum.x += v[k].x * f, sum.y += v[k].y * f, sum.z += v[k].z * f, sum.w += v[k].w * f, total += l[k] * f;
+      }
+    }
+    if (turn) __syncthreads();  // the sums of the turn before have been read
+    sums[set][lane] = sum, totals[set][lane] = total;
+    __syncthreads();
+    const uint64_t which = (uint64_t)(uint32_t)t.tile * NC + combo;
+    if (set == 0 && which < (uint64_t)s.rows * w.per) {
+#pragma unroll
+      for (int k = 1; k < kSets; ++k) {
+        const float4 v = sums[k][lane];
+        sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w, total += totals[k][lane];
+      }
+      const float inv = total > 0.f ? 1.0f / total : 0.f;
+      const int64_t to = ((s.first + (int64_t)(which / (uint32_t)w.per)) * w.q_heads + (int64_t)t.head * w.per + (int64_t)(which % (uint32_t)w.per)) * D + dim;
+      *reinterpret_cast<uint2*>(w.out + to) = make_uint2(pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv));
+    }
   }
-  const float inv = total > 0.f ? 1.0f / total : 0.f;
-  const int64_t to = ((s.first + (int64_t)(which / (uint32_t)w.per)) * w.q_heads + (int64_t)t.head * w.per + (int64_t)(which % (uint32_t)w.per)) * D + 4 * lane;
-  *reinterpret_cast<uint2*>(w.out + to) = make_uint2(pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv));
 }
 
 // Columns to a combination: as many of the groups as leave room for the combinations that a sequence has on average.
@@ -681,10 +708,14 @@ bool is_whole(int64_t most_keys) { return most_keys <= 1024; }
 
 }  // namespace
 
+// Workers of a launch that splits sequences: waves where there are many, else workgroups of four (three waves to a SIMD, and all at once).
+bool split_by_wave(int nc, int64_t segments) { return nc <= 8 && segments >= 256; }
+int64_t most_workers(int nc, int64_t segments) { return split_by_wave(nc, segments) ? kMostWorkers : kMostWorkers / 4; }
+
 size_t paged_attention_workspace(int head_dim, int64_t rows, int64_t q_heads, int64_t kv_heads, int64_t seqs, int64_t) {
   // (whatever max_keys says: a sequence may be longer)
-  const int64_t nc = 16 / columns_of(head_dim, rows, seqs, q_heads / kv_heads);
-  return ((kMostGroups * sizeof(PagedTail) + 255) & ~(size_t)255) + 2 * kMostGroups * nc * (head_dim + 2) * sizeof(float);
+  const int64_t nc = 16 / columns_of(head_dim, rows, seqs, q_heads / kv_heads), workers = most_workers((int)nc, seqs * kv_heads);
+  return ((workers * sizeof(PagedTail) + 255) & ~(size_t)255) + 2 * workers * nc * (head_dim + 2) * sizeof(float);
 }
 
 hipError_t launch_paged_attention(int scale_kind, bool asym, int head_dim, const PagedPool& pool, const uint16_t* q, int64_t rows,
@@ -698,32 +729,33 @@ hipError_t launch_paged_attention(int scale_kind, bool asym, int head_dim, const
   // at most so many tiles of combinations have all sequences together, and so many units
   const int64_t tiles = (rows * per / nc + (seqs < rows ? seqs : rows)) * pool.kv_heads, tokens = (width + kTile - 1) / kTile;
   int unit_log2 = 0;
-  while (tiles >= (int64_t(1) << 31) / ((tokens >> unit_log2) + 1)) ++unit_log2;
+  while (tiles >= (int64_t(1) << 31) / ((tokens >> unit_log2) + 1 + kStart)) ++unit_log2;
   const PagedWork w = {q, out, static_cast<uint8_t*>(workspace), rows, max_pages, (int)seqs, (int)q_heads, (int)per,
                        scale * 1.4426950408889634f, whole ? 1 : 0, unit_log2};
   const size_t values = 4 * kTile * (size_t)head_dim / 2, shares = 4 * (size_t)nc * head_dim * sizeof(float);
   const int64_t segments = seqs * pool.kv_heads;
-  const bool by_wave = whole && segments >= 512;
+  const bool by_wave = whole ? segments >= 512 : split_by_wave(nc, segments);
   dim3 grid;
-  size_t lds = values;
+  int64_t workers = 0;
+  size_t lds = by_wave || shares < values ? values : shares;
   if (whole) {
     // tiles of combinations of one sequence: as many as there are on average, at least
     const int64_t ct = (rows * per + seqs * nc - 1) / (seqs * nc);
     grid = dim3((unsigned)(by_wave ? (segments + 3) / 4 : segments), (unsigned)(ct < 1024 ? ct : 1024));
-    if (!by_wave && shares > values) lds = shares;
   } else {
-    const int64_t units = tiles * ((((most_keys + kTile - 1) / kTile) >> unit_log2) / 4 + 1);
-    grid = dim3((unsigned)(units < kMostGroups ? units : kMostGroups));
-    lds = (((size_t)seqs * 4 + 63) & ~(size_t)63) + (values > shares ? values : shares);
+    const int64_t units = tiles * ((((most_keys + kTile - 1) / kTile) >> unit_log2) + 1 + kStart) / 4 + 1, most = most_workers(nc, segments);
+    workers = (units < most ? units + 3 : most) & ~int64_t(3);
+    grid = dim3((unsigned)(by_wave ? workers / 4 : workers));
+    lds += ((size_t)seqs * 4 + 63) & ~(size_t)63;
   }
   auto go = [&]<int SK, bool ASYM, int D, int GC>() {
-    if (by_wave)
-      hipLaunchKernelGGL((paged_attention_kernel<SK, ASYM, D, GC, 1>), grid, dim3(256), lds, s, pool, w, table, lens, starts, positions);
-    else
+    if (!by_wave)
       hipLaunchKernelGGL((paged_attention_kernel<SK, ASYM, D, GC, 4>), grid, dim3(256), lds, s, pool, w, table, lens, starts, positions);
+    else
+      hipLaunchKernelGGL((paged_attention_kernel<SK, ASYM, D, GC, 1>), grid, dim3(256), lds, s, pool, w, table, lens, starts, positions);
     if (!whole)
-      hipLaunchKernelGGL((paged_attention_join_kernel<D, 16 / GC>), dim3(grid.x, 16 / GC), dim3(256), 0, s, w, pool.page_log2, lens, starts,
-                         grid.x);
+      hipLaunchKernelGGL((paged_attention_join_kernel<D, 16 / GC>), dim3((unsigned)workers), dim3(512), 0, s, w, pool.page_log2, lens, starts,
+                         (uint32_t)workers);
     return hipGetLastError();
   };
   auto with_format = [&]<int SK, bool ASYM>() {
