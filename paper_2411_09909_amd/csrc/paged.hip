@@ -294,7 +294,7 @@ int done(const char* what) {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? AMX_OK : report_hip_error(e, what);
 }
-constexpr int64_t kMaxTokens = int64_t(1) << 30, kMaxRows = int64_t(1) << 24, kMaxHeads = 1024;
+constexpr int64_t kMaxTokens = int64_t(1) << 30, kMaxRows = int64_t(1) << 24, kMaxHeads = 1024, kMaxQueries = int64_t(1) << 31;
 
 // log2 of a page size that is taken, else -1
 int page_log2(int64_t page_size) {
@@ -437,7 +437,7 @@ int amxfp4_paged_read(const amx_format_t* fmt, const amx_paged_pool_t* pool, con
 size_t amxfp4_paged_attention_workspace_bytes(const amx_format_t* fmt, const amx_paged_pool_t* pool, int64_t rows, int64_t q_heads,
                                               int64_t seqs, int64_t max_keys) {
   if (check(fmt, pool) != AMX_OK || rows <= 0 || rows > kMaxRows || q_heads <= 0 || q_heads > kMaxHeads || q_heads % pool->kv_heads ||
-      seqs <= 0 || seqs > kPagedMaxSeqs || max_keys < 0 || max_keys > kMaxTokens)
+      seqs <= 0 || seqs > kPagedMaxSeqs || max_keys < 0 || max_keys > kMaxTokens || rows * q_heads > kMaxQueries)
     return 0;
   return paged_attention_workspace(pool->head_dim, rows, q_heads, pool->kv_heads, seqs, max_keys);
 }
@@ -451,7 +451,8 @@ int amxfp4_paged_attention(const amx_format_t* fmt, const amx_paged_pool_t* pool
   if (!q_bf16 || !table || !lens || !starts || !positions || !out_bf16)
     return report_error(AMX_ERR_INVALID_ARG, "paged_attention: NULL pointer");
   if (rows <= 0 || rows > kMaxRows || q_heads <= 0 || q_heads > kMaxHeads || q_heads % pool->kv_heads || seqs <= 0 ||
-      seqs > kPagedMaxSeqs || max_pages <= 0 || max_pages > kMaxTokens / pool->page_size || max_keys < 0 || max_keys > kMaxTokens)
+      seqs > kPagedMaxSeqs || max_pages <= 0 || max_pages > kMaxTokens / pool->page_size || max_keys < 0 || max_keys > kMaxTokens ||
+      rows * q_heads > kMaxQueries)
     return report_error(AMX_ERR_INVALID_ARG, "paged_attention: bad shape (q_heads a multiple of kv_heads, 1 to 4096 sequences)");
   if (!(scale > 0.f) || isinf(scale)) return report_error(AMX_ERR_INVALID_ARG, "paged_attention: scale must be positive and finite");
   if (!aligned16(q_bf16) || !aligned16(out_bf16) || !aligned4(table) || !aligned4(lens) || !aligned4(starts) || !aligned4(positions))

@@ -41,7 +41,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short i16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTile = 64;        // tokens of a unit
-constexpr int kMostWorkers = 3072;
+constexpr int kMostWorkers = 768;  // of a launch that splits sequences: three workgroups to a compute unit, all at once
 // A sequence, key head and tile of combinations takes as long as this many tiles before its first one is in: the chain from the lengths
 // over the table to the keys, and the joining of the waves.
 constexpr uint32_t kStart = 12;
@@ -57,11 +57,11 @@ struct PagedWork {
   int whole, unit_log2;    // tiles of 64 tokens to a unit
 };
 
-// What a worker (a workgroup or a wave) leaves behind for the joining kernel, at the front of the workspace.
+// What a workgroup leaves behind for the joining kernel, at the front of the workspace.
 struct PagedTail {
-  uint32_t units, end;    // all units; one past the last of the sequence, key head and tile that this worker began and did not end
-  uint32_t groups, owner;  // workers among which the units are divided; 1: it began such a one
-  int32_t seq, head, tile, pad;
+  uint32_t units, end;    // all units; one past the last of the sequence, key head and tile that it began and did not end
+  uint32_t groups, owner;  // workgroups among which the units are divided; 1: it began such a one
+  uint32_t first, rows, head, tile;  // the sequence's rows; key head; tile of combinations
 };
 
 // units of a worker: [first_unit(g), first_unit(g + 1))
@@ -78,6 +78,11 @@ struct PagedSequence {
   uint32_t rows, keys, NT, CT;
 };
 template <int NC>
+__device__ __forceinline__ void paged_tiles(const PagedWork& w, PagedSequence& s) {
+  s.NT = max((s.keys + kTile - 1) / kTile, 1u);
+  s.CT = (s.rows * (uint32_t)w.per + NC - 1) / NC;  // (rows * q_heads <= 2^31)
+}
+template <int NC>
 __device__ __forceinline__ PagedSequence paged_sequence(const PagedWork& w, uint32_t page_log2, const int32_t* __restrict__ lens,
                                                         const int32_t* __restrict__ starts, int b) {
   PagedSequence s;
@@ -86,10 +91,13 @@ __device__ __forceinline__ PagedSequence paged_sequence(const PagedWork& w, uint
   s.first = a;
   s.rows = e > a ? (uint32_t)(e - a) : 0u;
   s.keys = (uint32_t)max(0, min(n, (int)(w.max_pages << page_log2)));  // (at most 2^30)
-  s.NT = max((s.keys + kTile - 1) / kTile, 1u);
-  s.CT = (uint32_t)(((uint64_t)s.rows * w.per + NC - 1) / NC);
+  paged_tiles<NC>(w, s);
   return s;
 }
+
+// LDS that a launch which splits sequences takes for them
+constexpr int kKept = 512;
+__host__ __device__ constexpr size_t sequences_bytes(int64_t seqs) { return ((size_t)seqs * (seqs <= kKept ? 16 : 4) + 63) & ~(size_t)63; }
 
 // max over the four quarters of a wave (lanes of the same column)
 __device__ __forceinline__ float quarters_max(float v) {
@@ -187,16 +195,20 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
   __shared__ float top_of[4][NC], sum_of[4][NC];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  uint32_t* const ends = reinterpret_cast<uint32_t*>(lds);  // split: units up to and with a sequence
-  uint8_t* const region = lds + (w.whole ? 0 : ((size_t)w.seqs * 4 + 63) & ~(size_t)63);
+  const bool whole = SHARE == 1 || w.whole;
+  // split: units up to and with a sequence; of up to kKept sequences also what paged_sequence() reads
+  uint32_t* const ends = reinterpret_cast<uint32_t*>(lds);
+  uint32_t* const kept = ends + w.seqs;
+  const bool keep = w.seqs <= kKept;
+  uint8_t* const region = lds + (whole ? 0 : sequences_bytes(w.seqs));
   uint8_t* const mine = region + wave * kValueBytes;
 
   int b, head;
   uint32_t ct = 0, unit = 0, hi = 0;
-  const uint32_t worker = SHARE == 1 ? blockIdx.x * 4 + wave : blockIdx.x, workers = SHARE == 1 ? gridDim.x * 4 : gridDim.x;
+  const uint32_t worker = SHARE == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
   // units of a sequence, key head and tile of combinations
   auto units_of = [&](uint32_t NT) { return kStart + ((NT + (1u << w.unit_log2) - 1) >> w.unit_log2); };
-  if (w.whole) {
+  if (whole) {
     if (worker >= (uint32_t)w.seqs * pool.kv_heads) return;  // (SHARE == 1: the wave; nobody waits for it)
     b = __builtin_amdgcn_readfirstlane((int)(worker / pool.kv_heads)), head = (int)worker - b * (int)pool.kv_heads;
     ct = blockIdx.y;
@@ -210,6 +222,7 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
     uint32_t sum = 0;
     for (int i = b0; i < b1; ++i) {
       const PagedSequence s = paged_sequence<NC>(w, pool.page_log2, lens, starts, i);
+      if (keep) kept[i] = (uint32_t)s.first, kept[w.seqs + i] = s.rows, kept[2 * w.seqs + i] = s.keys;
       const uint64_t own = min((uint64_t)s.CT * units_of(s.NT), (uint64_t)kMostUnits) * pool.kv_heads;
       ends[i] = sum = (uint32_t)min(sum + own, (uint64_t)kMostUnits);
     }
@@ -228,8 +241,8 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
     __syncthreads();
     const uint32_t units = __builtin_amdgcn_readfirstlane(ends[w.seqs - 1]);
     // four units at least
-    const uint32_t groups = max(1u, min(workers, w.unit_log2 ? units : (units + 3) / 4));
-    if ((threadIdx.x & (SHARE == 1 ? 63 : 255)) == 0) reinterpret_cast<PagedTail*>(w.workspace)[worker] = PagedTail{units, 0, groups, 0, 0, 0, 0, 0};
+    const uint32_t groups = max(1u, min((uint32_t)gridDim.x, w.unit_log2 ? units : (units + 3) / 4));
+    if (threadIdx.x == 0) reinterpret_cast<PagedTail*>(w.workspace)[worker] = PagedTail{units, 0, groups, 0, 0, 0, 0, 0};
     if (worker >= groups || units == 0) return;
     unit = first_unit(units, groups, worker), hi = first_unit(units, groups, worker + 1);
     // the first sequence whose units end behind the range's first: its 64th of the sequences, then in there
@@ -247,12 +260,19 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
     const int lane = thread & 63, r = lane & 15, u = lane >> 4, c = r / GC, gc = r % GC;
     uint32_t t0 = 0, t1, after = 0;  // tiles of tokens; the unit behind the segment's last
     bool complete = true;
-    if (!w.whole) {
+    if (!whole) {
       if (unit >= hi) return;
       while (__builtin_amdgcn_readfirstlane(ends[b]) <= unit) ++b;
     }
-    const PagedSequence s = paged_sequence<NC>(w, pool.page_log2, lens, starts, b);
-    if (w.whole) {
+    PagedSequence s;
+    if (!whole && keep) {
+      s.first = __builtin_amdgcn_readfirstlane(kept[b]), s.rows = __builtin_amdgcn_readfirstlane(kept[w.seqs + b]);
+      s.keys = __builtin_amdgcn_readfirstlane(kept[2 * w.seqs + b]);
+      paged_tiles<NC>(w, s);
+    } else {
+      s = paged_sequence<NC>(w, pool.page_log2, lens, starts, b);
+    }
+    if (whole) {
       if (ct >= s.CT) return;
       t1 = s.NT;
     } else {
@@ -272,15 +292,35 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
     const int32_t* row_table = table + (int64_t)b * w.max_pages;
     const uint32_t last_entry = (uint32_t)(w.max_pages - 1);
 
+    // ---- this lane's combination
+    const uint32_t combination = ct * NC + c;
+    const bool asked = combination < s.rows * (uint32_t)w.per;
+    const uint32_t row_of = asked ? combination / (uint32_t)w.per : 0u, head_of = asked ? combination - row_of * (uint32_t)w.per : 0u;
+    const int64_t row = s.first + row_of;
+    const int position = positions[row < w.rows ? row : 0];
+
+    // ---- the query: dimensions 32 j + 8 u .. of group j, zeros where the column is not the group's; where the keys' words stay as
+    // they are loaded (all groups in the columns), dimensions 32 u + 8 j .. of group u
+    u32x4 q[Tile::kGroups];
+#pragma unroll
+    for (int j = 0; j < Tile::kGroups; ++j) {
+      q[j] = u32x4{0, 0, 0, 0};
+      if (asked && (Tile::kAsLoaded ? u : j % GC) == gc)
+        q[j] = *reinterpret_cast<const u32x4*>(w.q + (row * w.q_heads + (int64_t)head * w.per + head_of) * D +
+                                               (Tile::kAsLoaded ? 32 * u + 8 * j : 32 * j + 8 * u));
+    }
+
     // ---- requests. A tile's registers take the next tile's data once they have been used: K, its scales and V (which is in LDS by
     // then) after the scores, V's scales after the weights.
     const int64_t page_stride = (int64_t)pool.kv_heads << pool.page_log2;
     const uint32_t mask = (1u << pool.page_log2) - 1;
-    // pages of the four sub-blocks of 16 tokens of the tile that is requested next (four variables: an array would be indexed)
-    uint32_t id0, id1, id2, id3;
-    auto look_up = [&](uint32_t tile) {
-      auto entry = [&](uint32_t k) { return (uint32_t)row_table[min((tile * kTile + 16 * k) >> pool.page_log2, last_entry)]; };
-      id0 = entry(0), id1 = entry(1), id2 = entry(2), id3 = entry(3);
+    // Pages of the four sub-blocks of 16 tokens of the tile that is requested next (four variables: an array would be indexed). Asked for a
+    // tile ahead, one to a lane, through the vector memory: a scalar load in flight would make every wait for LDS wait for it.
+    uint32_t id0, id1, id2, id3, ahead;
+    auto look_up = [&](uint32_t tile) { ahead = (uint32_t)row_table[min((tile * kTile + 16 * (lane & 3)) >> pool.page_log2, last_entry)]; };
+    auto found = [&]() {
+      id0 = (uint32_t)__builtin_amdgcn_readlane((int)ahead, 0), id1 = (uint32_t)__builtin_amdgcn_readlane((int)ahead, 1);
+      id2 = (uint32_t)__builtin_amdgcn_readlane((int)ahead, 2), id3 = (uint32_t)__builtin_amdgcn_readlane((int)ahead, 3);
     };
     auto in_pool = [&](uint32_t id) { return id < pool.pages ? id : 0u; };
     auto pick = [&](int k) {  // of a sub-block that depends on the lane
@@ -326,6 +366,7 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
     uint32_t tile = t0 + (SHARE == 1 ? 0 : wave), bad = 0;
     look_up(tile);
     if (tile < t1) {
+      found();
       bad = bad_pages();
       request_values(tile, d);
       request_keys(tile, d);
@@ -333,29 +374,13 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
     }
     look_up(tile + SHARE);
 
-    // ---- this lane's combination
-    const uint64_t combination = (uint64_t)ct * NC + c;
-    const bool asked = combination < (uint64_t)s.rows * w.per;
-    const uint32_t row_of = asked ? (uint32_t)(combination / (uint32_t)w.per) : 0u, head_of = asked ? (uint32_t)(combination % (uint32_t)w.per) : 0u;
-    const int64_t row = s.first + row_of;
     // tokens it sees; columns that nobody asked for see all and are not looked at
-    const int limit = asked ? min(max(positions[row], -1) + 1, (int)s.keys) : 0x7FFFFFFF;
+    const int limit = asked ? min(max(position, -1) + 1, (int)s.keys) : 0x7FFFFFFF;
     int least = limit, most = asked ? limit : 0;  // (the same in all quarters and in the columns of a combination)
 #pragma unroll
     for (int o = GC; o < 16; o <<= 1) least = min(least, __shfl_xor(least, o, 64)), most = max(most, __shfl_xor(most, o, 64));
     least = __builtin_amdgcn_readfirstlane(least), most = __builtin_amdgcn_readfirstlane(most);
     const uint32_t stop = min(t1, (uint32_t)(most + kTile - 1) / kTile);
-
-    // ---- the query: dimensions 32 j + 8 u .. of group j, zeros where the column is not the group's; where the keys' words stay as
-    // they are loaded (all groups in the columns), dimensions 32 u + 8 j .. of group u
-    u32x4 q[Tile::kGroups];
-#pragma unroll
-    for (int j = 0; j < Tile::kGroups; ++j) {
-      q[j] = u32x4{0, 0, 0, 0};
-      if (asked && (Tile::kAsLoaded ? u : j % GC) == gc)
-        q[j] = *reinterpret_cast<const u32x4*>(w.q + (row * w.q_heads + (int64_t)head * w.per + head_of) * D +
-                                               (Tile::kAsLoaded ? 32 * u + 8 * j : 32 * j + 8 * u));
-    }
 
     // ---- the tiles
     f32x4 o[DT];
@@ -427,6 +452,7 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
 #pragma unroll
       for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(x[i]));
       if (more) {
+        found();
         request_keys(tile + SHARE, d);
         request_values(tile + SHARE, d);
       }
@@ -545,41 +571,23 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
     asm volatile("" : "+v"(thread));
     const int to_u = (int)(thread & 63) >> 4, to_c = (int)(thread & 15) / GC, to_gc = (int)(thread & 15) % GC;
     // where a combination's result goes
-    auto destination = [&](uint64_t which) {
-      const uint32_t i = (uint32_t)(which / (uint32_t)w.per), h = (uint32_t)(which % (uint32_t)w.per);
+    auto destination = [&](uint32_t which) {
+      const uint32_t i = which / (uint32_t)w.per, h = which - i * (uint32_t)w.per;
       return w.out + ((s.first + i) * w.q_heads + (int64_t)head * w.per + h) * D;
     };
-    // where a part of one goes: slot 0, begun by another worker, or 1, begun here
-    auto part_of = [&]() {
-      return reinterpret_cast<float*>(w.workspace + (((size_t)workers * sizeof(PagedTail) + 255) & ~(size_t)255)) +
-             (2 * (size_t)worker + (t0 == 0 ? 1 : 0)) * kPartFloats<NC, D>;
-    };
-    auto leave_tail = [&]() {
-      PagedTail* tail = reinterpret_cast<PagedTail*>(w.workspace) + worker;
-      tail->end = after, tail->owner = 1, tail->seq = b, tail->head = head, tail->tile = (int32_t)ct;
-    };
     if constexpr (SHARE == 1) {
-      if (complete) {
-        const float inv = l > 0.f ? 1.0f / l : 0.f;
-        const uint64_t which = (uint64_t)ct * NC + to_c;
-        if (which < (uint64_t)s.rows * w.per) {
-          uint16_t* to = destination(which) + 4 * to_u;
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
-            if ((dt >> 1) % GC == to_gc) {
-              const f32x4 v = o[dt] * inv;
-              *reinterpret_cast<uint2*>(to + dt * 16) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-            }
-        }
-      } else {
-        float* part = part_of();
+      const float inv = l > 0.f ? 1.0f / l : 0.f;
+      const uint32_t which = ct * NC + to_c;
+      if (which < s.rows * (uint32_t)w.per) {
+        uint16_t* to = destination(which) + 4 * to_u;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
-          if ((dt >> 1) % GC == to_gc) *reinterpret_cast<f32x4*>(part + to_c * D + dt * 16 + 4 * to_u) = o[dt];
-        if (to_u == 0 && to_gc == 0) part[NC * D + to_c] = m * sc, part[NC * D + NC + to_c] = l;
-        if (t0 == 0 && (thread & 63) == 0) leave_tail();
+          if ((dt >> 1) % GC == to_gc) {
+            const f32x4 v = o[dt] * inv;
+            *reinterpret_cast<uint2*>(to + dt * 16) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+          }
       }
-      if (w.whole) ct += gridDim.y;
+      ct += gridDim.y;
       continue;
     }
 
@@ -593,7 +601,10 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
     for (int dt = 0; dt < DT; ++dt)
       if ((dt >> 1) % GC == to_gc) *reinterpret_cast<f32x4*>(share + wave * kShareFloats + to_c * D + dt * 16 + 4 * to_u) = o[dt] * factor;
     __syncthreads();
-    float* part = complete ? nullptr : part_of();
+    float* part = nullptr;
+    if (!complete)  // slot 0: begun by another worker, 1: begun here
+      part = reinterpret_cast<float*>(w.workspace + (((size_t)gridDim.x * sizeof(PagedTail) + 255) & ~(size_t)255)) +
+             (2 * (size_t)worker + (t0 == 0 ? 1 : 0)) * kPartFloats<NC, D>;
     for (int i = (int)thread; i < kShareFloats / 2; i += 256) {
       const int combo = 2 * i / D, dim = 2 * i % D;
       float2 v = *reinterpret_cast<const float2*>(share + 2 * i);
@@ -608,8 +619,8 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
 #pragma unroll
       for (int k = 0; k < 4; ++k) total += top_of[k][combo] == -INFINITY ? 0.f : sum_of[k][combo] * __builtin_amdgcn_exp2f((top_of[k][combo] - best) * sc);
       if (complete) {
-        const uint64_t which = (uint64_t)ct * NC + combo;
-        if (which < (uint64_t)s.rows * w.per) {
+        const uint32_t which = ct * NC + combo;
+        if (which < s.rows * (uint32_t)w.per) {
           const float inv = total > 0.f ? 1.0f / total : 0.f;
           *reinterpret_cast<uint32_t*>(destination(which) + dim) = pack_bf16(v.x * inv, v.y * inv);
         }
@@ -618,10 +629,12 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
         if (dim == 0) part[NC * D + combo] = best * sc, part[NC * D + NC + combo] = total;
       }
     }
-    if (w.whole)
+    if (whole) {
       ct += gridDim.y;
-    else if (!complete && t0 == 0 && threadIdx.x == 0)
-      leave_tail();
+    } else if (!complete && t0 == 0 && threadIdx.x == 0) {
+      PagedTail* tail = reinterpret_cast<PagedTail*>(w.workspace) + worker;
+      tail->end = after, tail->owner = 1, tail->first = (uint32_t)s.first, tail->rows = s.rows, tail->head = (uint32_t)head, tail->tile = ct;
+    }
     __syncthreads();  // the share has been read
   }
 }
@@ -630,13 +643,12 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
 // the first slots of those after it, in their order. One workgroup to a worker of the other kernel; most have nothing to do. A part's floats
 // are shared out over `kLanes` threads, the parts over the rest, eight requests of each under way at once.
 template <int D, int NC>
-__global__ __launch_bounds__(512) void paged_attention_join_kernel(PagedWork w, uint32_t page_log2, const int32_t* __restrict__ lens,
-                                                                   const int32_t* __restrict__ starts, uint32_t workers) {
-  constexpr int kLanes = NC * D / 4 < 512 ? NC * D / 4 : 512, kSets = 512 / kLanes, kTurns = NC * D / 4 / kLanes;
+__global__ __launch_bounds__(512) void paged_attention_join_kernel(PagedWork w, uint32_t workers) {
+  constexpr int kLanes = NC * D / 4, kSets = 512 / kLanes;
+  static_assert(kLanes <= 512, "one pass");
   const uint32_t g = blockIdx.x;
   const PagedTail t = reinterpret_cast<const PagedTail*>(w.workspace)[g];
   if (!t.owner) return;
-  const PagedSequence s = paged_sequence<NC>(w, page_log2, lens, starts, t.seq);
   // the worker that has the segment's last unit: about (end - 1) groups / units
   uint32_t last = (uint32_t)((uint64_t)(t.end - 1) * t.groups / t.units);
   last = min(last, t.groups - 1);
@@ -645,55 +657,55 @@ __global__ __launch_bounds__(512) void paged_attention_join_kernel(PagedWork w, 
   const uint32_t count = last - g + 1;
   const float* parts = reinterpret_cast<const float*>(w.workspace + (((size_t)workers * sizeof(PagedTail) + 255) & ~(size_t)255));
   auto part = [&](uint32_t i) { return parts + (2 * (size_t)(g + i) + (i == 0 ? 1 : 0)) * kPartFloats<NC, D>; };
-  __shared__ float tops[8][NC];
   __shared__ float4 sums[kSets][kLanes];
-  __shared__ float totals[kSets][kLanes];
-  // the combinations' largest: thread (part, combination)
-  constexpr int kEach = 512 / NC;
-  float top = -INFINITY;
-  for (uint32_t i = threadIdx.x / NC; i < count; i += kEach) top = fmaxf(top, part(i)[NC * D + threadIdx.x % NC]);
+  __shared__ float2 rest[kSets][kLanes];
+  const int set = threadIdx.x / kLanes, lane = threadIdx.x % kLanes, combo = lane / (D / 4), dim = 4 * (lane % (D / 4));
+  float4 sum = make_float4(0, 0, 0, 0);
+  float total = 0.f, top = -INFINITY;
+  // a set's parts, against their own running maximum
+  for (uint32_t i0 = set; i0 < count; i0 += 8 * kSets) {
+    float4 v[8];
+    float m[8], l[8], best = top;
 #pragma unroll
-  for (int o = NC; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-  if ((threadIdx.x & 63) < NC) tops[threadIdx.x >> 6][threadIdx.x & 63] = top;
-  __syncthreads();
-  const int set = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
-#pragma unroll
-  for (int turn = 0; turn < kTurns; ++turn) {
-    const int item = turn * kLanes + lane, combo = item / (D / 4), dim = 4 * (item % (D / 4));
-    float best = tops[0][combo];
-#pragma unroll
-    for (int k = 1; k < 8; ++k) best = fmaxf(best, tops[k][combo]);
-    float4 sum = make_float4(0, 0, 0, 0);
-    float total = 0.f;
-    for (uint32_t i0 = set; i0 < count; i0 += 8 * kSets) {
-      float4 v[8];
-      float m[8], l[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float* p = part(min(i0 + k * kSets, count - 1));
-        v[k] = *reinterpret_cast<const float4*>(p + 4 * item), m[k] = p[NC * D + combo], l[k] = p[NC * D + NC + combo];
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float f = i0 + k * kSets >= count || m[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[k] - best);
-        sum.x += v[k].x * f, sum.y += v[k].y * f, sum.z += v[k].z * f, sum.w += v[k].w * f, total += l[k] * f;
-      }
+    for (int k = 0; k < 8; ++k) {
+      const float* p = part(min(i0 + k * kSets, count - 1));
+      v[k] = *reinterpret_cast<const float4*>(p + 4 * lane), m[k] = p[NC * D + combo], l[k] = p[NC * D + NC + combo];
     }
-    if (turn) __syncthreads();  // the sums of the turn before have been read
-    sums[set][lane] = sum, totals[set][lane] = total;
-    __syncthreads();
-    const uint64_t which = (uint64_t)(uint32_t)t.tile * NC + combo;
-    if (set == 0 && which < (uint64_t)s.rows * w.per) {
 #pragma unroll
-      for (int k = 1; k < kSets; ++k) {
-        const float4 v = sums[k][lane];
-        sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w, total += totals[k][lane];
-      }
-      const float inv = total > 0.f ? 1.0f / total : 0.f;
-      const int64_t to = ((s.first + (int64_t)(which / (uint32_t)w.per)) * w.q_heads + (int64_t)t.head * w.per + (int64_t)(which % (uint32_t)w.per)) * D + dim;
-      *reinterpret_cast<uint2*>(w.out + to) = make_uint2(pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv));
+    for (int k = 0; k < 8; ++k) {
+      if (i0 + k * kSets >= count) m[k] = -INFINITY;
+      best = fmaxf(best, m[k]);
+    }
+    const float to = best == -INFINITY ? 0.f : best, old = __builtin_amdgcn_exp2f(top - to);
+    top = best;
+    sum.x *= old, sum.y *= old, sum.z *= old, sum.w *= old, total *= old;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (m[k] == -INFINITY) continue;  // (one that saw no key, or none)
+      const float f = __builtin_amdgcn_exp2f(m[k] - to);
+      sum.x += v[k].x * f, sum.y += v[k].y * f, sum.z += v[k].z * f, sum.w += v[k].w * f, total += l[k] * f;
     }
   }
+  sums[set][lane] = sum, rest[set][lane] = make_float2(top, total);
+  __syncthreads();
+  const uint32_t which = t.tile * NC + combo;
+  if (set != 0 || which >= t.rows * (uint32_t)w.per) return;
+  float best = top;
+#pragma unroll
+  for (int k = 1; k < kSets; ++k) best = fmaxf(best, rest[k][lane].x);
+  float4 all = make_float4(0, 0, 0, 0);
+  total = 0.f;
+#pragma unroll
+  for (int k = 0; k < kSets; ++k) {
+    const float4 v = sums[k][lane];
+    const float2 ml = rest[k][lane];
+    const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - best);
+    all.x += v.x * f, all.y += v.y * f, all.z += v.z * f, all.w += v.w * f, total += ml.y * f;
+  }
+  const float inv = total > 0.f ? 1.0f / total : 0.f;
+  const uint32_t i = which / (uint32_t)w.per, h = which - i * (uint32_t)w.per;
+  uint16_t* to = w.out + (((int64_t)t.first + i) * w.q_heads + (int64_t)t.head * w.per + h) * D + dim;
+  *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16(all.x * inv, all.y * inv), pack_bf16(all.z * inv, all.w * inv));
 }
 
 // Columns to a combination: as many of the groups as leave room for the combinations that a sequence has on average.
@@ -708,13 +720,9 @@ bool is_whole(int64_t most_keys) { return most_keys <= 1024; }
 
 }  // namespace
 
-// Workers of a launch that splits sequences: waves where there are many, else workgroups of four (three waves to a SIMD, and all at once).
-bool split_by_wave(int nc, int64_t segments) { return nc <= 8 && segments >= 256; }
-int64_t most_workers(int nc, int64_t segments) { return split_by_wave(nc, segments) ? kMostWorkers : kMostWorkers / 4; }
-
 size_t paged_attention_workspace(int head_dim, int64_t rows, int64_t q_heads, int64_t kv_heads, int64_t seqs, int64_t) {
   // (whatever max_keys says: a sequence may be longer)
-  const int64_t nc = 16 / columns_of(head_dim, rows, seqs, q_heads / kv_heads), workers = most_workers((int)nc, seqs * kv_heads);
+  const int64_t nc = 16 / columns_of(head_dim, rows, seqs, q_heads / kv_heads), workers = kMostWorkers;
   return ((workers * sizeof(PagedTail) + 255) & ~(size_t)255) + 2 * workers * nc * (head_dim + 2) * sizeof(float);
 }
 
@@ -734,7 +742,7 @@ hipError_t launch_paged_attention(int scale_kind, bool asym, int head_dim, const
                        scale * 1.4426950408889634f, whole ? 1 : 0, unit_log2};
   const size_t values = 4 * kTile * (size_t)head_dim / 2, shares = 4 * (size_t)nc * head_dim * sizeof(float);
   const int64_t segments = seqs * pool.kv_heads;
-  const bool by_wave = whole ? segments >= 512 : split_by_wave(nc, segments);
+  const bool by_wave = whole && segments >= 1024;
   dim3 grid;
   int64_t workers = 0;
   size_t lds = by_wave || shares < values ? values : shares;
@@ -743,10 +751,10 @@ hipError_t launch_paged_attention(int scale_kind, bool asym, int head_dim, const
     const int64_t ct = (rows * per + seqs * nc - 1) / (seqs * nc);
     grid = dim3((unsigned)(by_wave ? (segments + 3) / 4 : segments), (unsigned)(ct < 1024 ? ct : 1024));
   } else {
-    const int64_t units = tiles * ((((most_keys + kTile - 1) / kTile) >> unit_log2) + 1 + kStart) / 4 + 1, most = most_workers(nc, segments);
-    workers = (units < most ? units + 3 : most) & ~int64_t(3);
-    grid = dim3((unsigned)(by_wave ? workers / 4 : workers));
-    lds += ((size_t)seqs * 4 + 63) & ~(size_t)63;
+    const int64_t units = tiles * ((((most_keys + kTile - 1) / kTile) >> unit_log2) + 1 + kStart) / 4 + 1;
+    workers = units < kMostWorkers ? units : kMostWorkers;
+    grid = dim3((unsigned)workers);
+    lds += sequences_bytes(seqs);
   }
   auto go = [&]<int SK, bool ASYM, int D, int GC>() {
     if (!by_wave)
@@ -754,8 +762,7 @@ hipError_t launch_paged_attention(int scale_kind, bool asym, int head_dim, const
     else
       hipLaunchKernelGGL((paged_attention_kernel<SK, ASYM, D, GC, 1>), grid, dim3(256), lds, s, pool, w, table, lens, starts, positions);
     if (!whole)
-      hipLaunchKernelGGL((paged_attention_join_kernel<D, 16 / GC>), dim3((unsigned)workers), dim3(512), 0, s, w, pool.page_log2, lens, starts,
-                         (uint32_t)workers);
+      hipLaunchKernelGGL((paged_attention_join_kernel<D, 16 / GC>), dim3((unsigned)workers), dim3(512), 0, s, w, (uint32_t)workers);
     return hipGetLastError();
   };
   auto with_format = [&]<int SK, bool ASYM>() {

@@ -107,7 +107,7 @@ def test_attention(lib):
         return lib.amxfp4_paged_attention(ctypes.byref(f), ctypes.byref(p), q, rows, heads, table, seqs, width, lens, starts, positions,
                                           scale, keys, out, ws, size, None)
     for kw in (dict(q=None), dict(table=None), dict(lens=None), dict(starts=None), dict(positions=None), dict(out=None), dict(rows=0),
-               dict(rows=(1 << 24) + 1), dict(heads=12), dict(heads=0), dict(heads=2048), dict(seqs=0), dict(seqs=4097), dict(width=0),
+               dict(rows=(1 << 24) + 1), dict(heads=12), dict(heads=0), dict(rows=1 << 24, heads=136), dict(heads=2048), dict(seqs=0), dict(seqs=4097), dict(width=0),
                dict(width=(1 << 24) + 1), dict(keys=-1), dict(keys=(1 << 30) + 1), dict(scale=0.0), dict(scale=-1.0),
                dict(scale=float("nan")), dict(scale=float("inf")), dict(q=ctypes.c_void_p(0x1008)), dict(out=ctypes.c_void_p(0x1008)),
                dict(table=ODD), dict(lens=ODD), dict(starts=ODD), dict(positions=ODD)):
