@@ -14,19 +14,27 @@ namespace {
 
 // ---- bookkeeping ----------------------------------------------------------------------------------------------------
 
-// Inclusive prefix sums over 256 threads that stay at `cap` once they reach it (cap + cap fits; min(a + b, cap) is associative).
-__device__ __forceinline__ uint32_t scan_capped(uint32_t v, uint32_t cap, uint32_t* waves) {
+// Three inclusive prefix sums over 256 threads that stay at their caps once they reach them (cap + cap fits; min(a + b, cap) is
+// associative); before: the sums up to the thread before.
+struct Sums {
+  uint32_t rows, given, want;
+};
+__device__ __forceinline__ Sums add_capped(Sums a, Sums b, Sums cap) {
+  return {min(a.rows + b.rows, cap.rows), min(a.given + b.given, cap.given), min(a.want + b.want, cap.want)};
+}
+__device__ __forceinline__ Sums scan_before(Sums v, Sums cap, Sums* waves) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t u = __shfl_up(v, o, 64);
-    if (lane >= o) v = v + u < cap ? v + u : cap;
+    const Sums u = {__shfl_up(v.rows, o, 64), __shfl_up(v.given, o, 64), __shfl_up(v.want, o, 64)};
+    if (lane >= o) v = add_capped(v, u, cap);
   }
-  __syncthreads();  // `waves` may still be read from the scan before
   if (lane == 63) waves[wave] = v;
+  Sums before = {__shfl_up(v.rows, 1, 64), __shfl_up(v.given, 1, 64), __shfl_up(v.want, 1, 64)};
+  if (lane == 0) before = {0, 0, 0};
   __syncthreads();
-  for (int w = 0; w < wave; ++w) v = v + waves[w] < cap ? v + waves[w] : cap;
-  return v;
+  for (int w = 0; w < wave; ++w) before = add_capped(before, waves[w], cap);
+  return before;
 }
 
 // the first of n ascending numbers that is greater than x, n if none is
@@ -45,6 +53,13 @@ __device__ __forceinline__ int first_above(const uint32_t* v, int n, uint32_t x)
 // Every workgroup works out the sums over the sequences for itself (a few words a thread, out of the caches), then takes its
 // share of the rows and of the pages given back: one launch, and no workgroup waits for another. What is read (lens, state, the
 // queue's entries in use, table entries of pages held) is nowhere written.
+// One scan does for all: a sequence that ends behind the batch's last row is refused, and so are all after it, so what they would have
+// taken changes nothing.
+// Bound by the chain of one load, the scan and one more load, not by bytes: 4.7 us for 64 sequences of a token each, 8.8 us for 1000
+// sequences with 28000 rows. The rows of a sequence with few of them (decoding) are written by the thread that has the sequence; those
+// of longer ones are shared out, a row to a thread, each finding its sequence in the sums. With the search for all rows, a scan to each
+// sum and four rows to a thread the same took 6.4 and 13.3 us.
+constexpr int kDirectRows = 8;
 __global__ __launch_bounds__(256) void paged_plan_kernel(const int32_t* __restrict__ lens, const int32_t* __restrict__ new_rows,
                                                          int seqs, uint32_t rows, int page_log2, uint32_t pages,
                                                          uint32_t max_pages, const int32_t* __restrict__ state,
@@ -52,83 +67,90 @@ __global__ __launch_bounds__(256) void paged_plan_kernel(const int32_t* __restri
                                                          int32_t* __restrict__ starts, int32_t* __restrict__ slots,
                                                          int32_t* __restrict__ positions, int32_t* __restrict__ state_out) {
   extern __shared__ uint32_t sums[];
-  __shared__ uint32_t waves[4], taken_of[4], refused_of[4];
+  __shared__ Sums waves[4];
+  __shared__ uint32_t taken_of[4], refused_of[4], shared_out;
   uint32_t* ends = sums;                  // rows up to and with the sequence
-  uint32_t* first = sums + seqs;          // pages taken before it, kRefused if it is refused or has no rows
+  uint32_t* first = sums + seqs;          // its new rows; then: pages taken before it, kRefused if it is refused or has no rows
   uint32_t* back = sums + 2 * seqs;       // pages given back up to and with it
+  uint32_t* held_in = sums + 3 * seqs;    // the tokens it has
   constexpr uint32_t kRefused = ~0u;
   const uint32_t most = max_pages << page_log2, page_mask = (1u << page_log2) - 1;
-  const uint32_t head = (uint32_t)state[0] % pages;
-  const uint32_t count = state[1] < 0 ? 0u : min((uint32_t)state[1], pages);
   const int each = (seqs + 255) >> 8, b0 = threadIdx.x * each, b1 = min(seqs, b0 + each);
-  auto held = [&](int b) { return lens[b] < 0 ? 0u : min((uint32_t)lens[b], most); };
+  auto held_of = [&](int len) { return len < 0 ? 0u : min((uint32_t)len, most); };
   auto pages_of = [&](uint32_t tokens) { return (tokens + page_mask) >> page_log2; };
+  const Sums cap = {rows + 1, pages, pages + 1};
+  auto sums_of = [&](uint32_t held, int n) {
+    const bool room = n > 0 && (uint32_t)n <= most - held;
+    const uint32_t more = n > 0 ? (uint32_t)n : 0u, given = n < 0 ? pages_of(held) : 0u;
+    const uint32_t want = room ? pages_of(held + more) - pages_of(held) : 0u;
+    return add_capped(Sums{more < cap.rows ? more : cap.rows, given, want < cap.want ? want : cap.want}, Sums{0, 0, 0}, cap);
+  };
+  for (int b = threadIdx.x; b < seqs; b += 256) held_in[b] = held_of(lens[b]), first[b] = (uint32_t)new_rows[b];
+  const int32_t state0 = state[0], state1 = state[1];
+  if (threadIdx.x == 0) shared_out = 0;
+  __syncthreads();
+  Sums mine = {0, 0, 0};
+  for (int b = b0; b < b1; ++b) mine = add_capped(mine, sums_of(held_in[b], (int)first[b]), cap);
+  Sums upto = scan_before(mine, cap, waves);
+  const uint32_t head = (uint32_t)state0 % pages, count = state1 < 0 ? 0u : min((uint32_t)state1, pages);
 
-  uint32_t sum = 0, given = 0;
+  auto place = [&](uint32_t t, int b, uint32_t held, uint32_t before, uint32_t i) {  // row t: the sequence's i-th new one
+    const uint32_t p = held + i, number = p >> page_log2, old = pages_of(held);
+    int32_t* entry = table + (int64_t)b * max_pages + number;
+    int32_t page;
+    if (number >= old) {
+      page = queue[(head + (before + number - old)) % pages];
+      if ((p & page_mask) == 0) *entry = page;
+    } else {
+      page = *entry;
+    }
+    positions[t] = (int32_t)p;
+    // (an id outside the pool has no slot)
+    slots[t] = (uint32_t)page < pages ? (int32_t)(((uint32_t)page << page_log2) + (p & page_mask)) : -1;
+  };
+  uint32_t taken = 0, refused = 0;
   for (int b = b0; b < b1; ++b) {
-    const int n = new_rows[b];
-    sum = min(sum + min((uint32_t)max(n, 0), rows + 1), rows + 1);
-    given = min(given + (n < 0 ? pages_of(held(b)) : 0u), pages);
-    ends[b] = sum, back[b] = given;
-  }
-  const uint32_t sum_here = scan_capped(sum, rows + 1, waves), given_here = scan_capped(given, pages, waves);
-  // what lies before this thread's sequences: the sums up to the thread before
-  __shared__ uint32_t edge[256], edge2[256];
-  edge[threadIdx.x] = sum_here, edge2[threadIdx.x] = given_here;
-  __syncthreads();
-  const uint32_t sum_before = threadIdx.x ? edge[threadIdx.x - 1] : 0, given_before = threadIdx.x ? edge2[threadIdx.x - 1] : 0;
-  uint32_t want = 0;
-  for (int b = b0; b < b1; ++b) {
-    ends[b] = min(ends[b] + sum_before, rows + 1);
-    back[b] = min(back[b] + given_before, pages);
-    const int n = new_rows[b];
-    const uint32_t h = held(b);
-    const bool fits = n > 0 && (uint32_t)n <= most - h && ends[b] <= rows;
-    const uint32_t w = fits ? pages_of(h + n) - pages_of(h) : 0u;
-    first[b] = fits ? w : kRefused;
-    want = min(want + w, pages + 1);
-  }
-  const uint32_t want_here = scan_capped(want, pages + 1, waves);
-  __syncthreads();
-  edge[threadIdx.x] = want_here;
-  __syncthreads();
-  uint32_t upto = threadIdx.x ? edge[threadIdx.x - 1] : 0, taken = 0, refused = 0;
-  for (int b = b0; b < b1; ++b) {
-    const uint32_t w = first[b];
-    const bool fits = w != kRefused;
-    const uint32_t before = upto;
-    if (fits) upto = min(upto + w, pages + 1);
-    const bool ok = fits && (w == 0 || upto <= count);
-    if (upto <= count) taken = upto;
-    first[b] = ok ? before : kRefused;
-    refused += !ok && new_rows[b] > 0;
+    const int n = (int)first[b];
+    const uint32_t held = held_in[b];
+    const Sums own = sums_of(held, n), now = add_capped(upto, own, cap);
+    const bool fits = n > 0 && (uint32_t)n <= most - held && now.rows <= rows, ok = fits && (own.want == 0 || now.want <= count);
+    if (ok && now.want <= count) taken = now.want;  // (behind one refused for its pages the sum stays above count)
+    refused += n > 0 && !ok;
+    ends[b] = now.rows, first[b] = ok ? upto.want : kRefused, back[b] = now.given;
+    // rows of the last sequence that is cut off end with the batch
+    const uint32_t begin = min(upto.rows, rows), end = min(now.rows, rows);
+    if (end - begin > kDirectRows) {
+      shared_out = 1;
+    } else if ((uint32_t)(b - b0) % gridDim.x == blockIdx.x) {
+      for (uint32_t t = begin; t < end; ++t) {
+        if (ok)
+          place(t, b, held, upto.want, t - begin);
+        else
+          slots[t] = -1, positions[t] = -1;
+      }
+    }
+    if (blockIdx.x == 0) {
+      lens_out[b] = n < 0 ? 0 : (int32_t)(held + (ok ? (uint32_t)n : 0u));
+      starts[b + 1] = (int32_t)end;
+    }
+    upto = now;
   }
   __syncthreads();
 
   const uint32_t total = min(ends[seqs - 1], rows);
   const uint32_t stride = gridDim.x * 256u, me = blockIdx.x * 256u + threadIdx.x;
-  for (uint64_t t64 = me; t64 < rows; t64 += stride) {
-    const uint32_t t = (uint32_t)t64;
-    int32_t pos = -1, slot = -1;
-    if (t < total) {
-      const int b = first_above(ends, seqs, t);
-      const uint32_t begin = first[b];
-      if (begin != kRefused) {
-        const uint32_t h = held(b), p = h + (t - (b ? ends[b - 1] : 0)), number = p >> page_log2, old = pages_of(h);
-        int32_t* entry = table + (int64_t)b * max_pages + number;
-        int32_t page;
-        if (number >= old) {
-          page = queue[(head + (begin + number - old)) % pages];
-          if ((p & page_mask) == 0) *entry = page;
-        } else {
-          page = *entry;
-        }
-        pos = (int32_t)p;
-        // (an id outside the pool has no slot)
-        slot = (uint32_t)page < pages ? (int32_t)(((uint32_t)page << page_log2) + (p & page_mask)) : -1;
-      }
+  for (uint64_t t = (shared_out ? 0 : total) + (uint64_t)me; t < rows; t += stride) {
+    if (t >= total) {
+      slots[t] = -1, positions[t] = -1;
+      continue;
     }
-    slots[t] = slot, positions[t] = pos;
+    const int b = first_above(ends, seqs, (uint32_t)t);
+    const uint32_t begin = b ? ends[b - 1] : 0u, end = min(ends[b], rows);
+    if (end - begin <= kDirectRows) continue;  // its sequence's thread has written it
+    if (first[b] != kRefused)
+      place((uint32_t)t, b, held_in[b], first[b], (uint32_t)t - begin);
+    else
+      slots[t] = -1, positions[t] = -1;
   }
   const uint32_t given_all = min(back[seqs - 1], pages - count);
   for (uint32_t i = me; i < given_all; i += stride) {
@@ -137,11 +159,6 @@ __global__ __launch_bounds__(256) void paged_plan_kernel(const int32_t* __restri
     queue[(head + count + i) % pages] = table[(int64_t)b * max_pages + p];
   }
   if (blockIdx.x != 0) return;
-  for (int b = threadIdx.x; b < seqs; b += 256) {
-    const int n = new_rows[b];
-    lens_out[b] = n < 0 ? 0 : (int32_t)(held(b) + (first[b] != kRefused ? (uint32_t)n : 0u));
-    starts[b + 1] = (int32_t)min(ends[b], rows);
-  }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     taken = max(taken, (uint32_t)__shfl_xor(taken, o, 64));
@@ -161,59 +178,79 @@ __global__ __launch_bounds__(256) void paged_plan_kernel(const int32_t* __restri
 
 // The work is cut as in rope_quantize_kernel (layer_ops.hip): items of (row, head, run of 8 dimensions below head_dim / 2 and
 // the 8 head_dim / 2 further on), four neighbouring threads to a group of 32; the workgroup's threads first work out the FP64
-// sines and cosines of its rows. Heads 0 .. q_heads - 1 are queries, the next kv_heads keys, the rest values. Same
-// arithmetic as split_heads_rope_kernel and the cast: same bits.
-constexpr int kWriteRows = 4, kWriteHeads = 16;
+// sines and cosines of its rows, while the loads of their first items are under way. Heads 0 .. q_heads - 1 are queries, the next
+// kv_heads keys, the rest values. Same arithmetic as split_heads_rope_kernel and the cast: same bits.
+// A thread keeps its row and run and goes from head to head, so that a sine and cosine leaves the LDS once.
+// `per_group` heads to a workgroup: with few rows the eight of one go (sixteen of 64 dimensions), so that there are workgroups enough
+// (1 row of 48 heads 3.7 us against 5.2 with all heads, 256 rows of 80 heads 6.0 against 9.6); with many all of them, so that the
+// angles are worked out once: 9500 rows of 48 heads 66 us against 68, 330 MB read and written at 5.0 TB/s.
+constexpr int kWriteRows = 4, kWriteManyGroups = 512;
+__device__ __forceinline__ uint32_t pack_rne(float a, float b) {
+  typedef __bf16 bf16_2 __attribute__((ext_vector_type(2)));
+  typedef float float_2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((float_2{a, b}), bf16_2));
+}
 template <int SCALE_KIND, bool ASYM, int D>
 __global__ __launch_bounds__(256) void paged_write_kernel(const float* __restrict__ in, int64_t rows, int64_t ld, int q_heads,
                                                           const int32_t* __restrict__ slots, const int32_t* __restrict__ positions,
-                                                          double log_theta, uint16_t* __restrict__ q_out, PagedPool pool) {
+                                                          double log_theta, int per_group, uint16_t* __restrict__ q_out, PagedPool pool) {
   constexpr int kHalf = D / 2, kRuns = D / 16;
   __shared__ double2 turn[kWriteRows * kHalf];  // dimension 8 j + e of row t at [e][t][j]
   const int heads = q_heads + 2 * (int)pool.kv_heads;
-  const int h0 = blockIdx.y * kWriteHeads, nh = min(heads - h0, kWriteHeads);
+  const int h0 = blockIdx.y * per_group, nh = min(heads - h0, per_group);
   const int64_t t0 = (int64_t)blockIdx.x * kWriteRows;
   const int nt = (int)min(rows - t0, (int64_t)kWriteRows);
   const int turned = q_heads + (int)pool.kv_heads;
+  const int j = threadIdx.x % kRuns, t = threadIdx.x / kRuns % kWriteRows;
+  constexpr int kHeads = 256 / (kRuns * kWriteRows);  // of one go
+  const int first = threadIdx.x / (kRuns * kWriteRows), last = t < nt ? h0 + nh : 0;
+  float4 next[4];
+  const float* row_in = in + (t0 + min(t, nt - 1)) * ld + 8 * j;
+  auto request = [&](int h) {  // (past the last head: the last one again, not used)
+    const float* p = row_in + (int64_t)min(h, heads - 1) * D;
+    next[0] = *reinterpret_cast<const float4*>(p), next[1] = *reinterpret_cast<const float4*>(p + 4);
+    next[2] = *reinterpret_cast<const float4*>(p + kHalf), next[3] = *reinterpret_cast<const float4*>(p + kHalf + 4);
+  };
+  request(h0 + first);
   if (h0 < turned)
     for (int a = threadIdx.x; a < nt * kHalf; a += 256) {
-      const int t = a / kHalf, i = a % kHalf;
-      const double ang = (double)positions[t0 + t] * exp(-log_theta * (double)i / (double)kHalf);
+      const int ta = a / kHalf, i = a % kHalf;
+      const int32_t pos = positions[t0 + ta];
+      const double inv = exp(-log_theta * (double)i / (double)kHalf);
       double sn, cs;
-      sincos(ang, &sn, &cs);
-      turn[(i & 7) * (kWriteRows * kRuns) + t * kRuns + (i >> 3)] = make_double2(sn, cs);
+      sincos((double)pos * inv, &sn, &cs);
+      turn[(i & 7) * (kWriteRows * kRuns) + ta * kRuns + (i >> 3)] = make_double2(sn, cs);
     }
   __syncthreads();
   const uint64_t size = (uint64_t)pool.pages << pool.page_log2;
-  for (int it = threadIdx.x; it < nt * nh * kRuns; it += 256) {
-    const int j = it % kRuns, th = it / kRuns, t = th / nh, h = h0 + th % nh;  // (the same t and h for the four threads of a group)
-    const float* p = in + (t0 + t) * ld + (int64_t)h * D + 8 * j;
-    float x1[8], x2[8];
+  double2 r[8];
+  int32_t position = 0, slot = -1;
+  if (t < nt) {
+    position = positions[t0 + t], slot = slots[t0 + t];
 #pragma unroll
-    for (int e = 0; e < 8; e += 4) {
-      const float4 a = *reinterpret_cast<const float4*>(p + e), b = *reinterpret_cast<const float4*>(p + kHalf + e);
-      x1[e] = a.x, x1[e + 1] = a.y, x1[e + 2] = a.z, x1[e + 3] = a.w;
-      x2[e] = b.x, x2[e + 1] = b.y, x2[e + 2] = b.z, x2[e + 3] = b.w;
-    }
+    for (int e = 0; e < 8; ++e) r[e] = turn[e * (kWriteRows * kRuns) + t * kRuns + j];
+  }
+  for (int h = h0 + first; h < last; h += kHeads) {  // (the same h for the four threads of a group)
+    float x1[8] = {next[0].x, next[0].y, next[0].z, next[0].w, next[1].x, next[1].y, next[1].z, next[1].w};
+    float x2[8] = {next[2].x, next[2].y, next[2].z, next[2].w, next[3].x, next[3].y, next[3].z, next[3].w};
+    if (h + kHeads < last) request(h + kHeads);
     if (h < turned) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const double2 r = turn[e * (kWriteRows * kRuns) + t * kRuns + j];
         const float a = x1[e], b = x2[e];
-        x1[e] = (float)((double)a * r.y - (double)b * r.x);
-        x2[e] = (float)((double)b * r.y + (double)a * r.x);
+        x1[e] = (float)((double)a * r[e].y - (double)b * r[e].x);
+        x2[e] = (float)((double)b * r[e].y + (double)a * r[e].x);
       }
     }
-    const uint32_t d1[4] = {pack2(x1[0], x1[1]), pack2(x1[2], x1[3]), pack2(x1[4], x1[5]), pack2(x1[6], x1[7])};
-    const uint32_t d2[4] = {pack2(x2[0], x2[1]), pack2(x2[2], x2[3]), pack2(x2[4], x2[5]), pack2(x2[6], x2[7])};
+    const uint32_t d1[4] = {pack_rne(x1[0], x1[1]), pack_rne(x1[2], x1[3]), pack_rne(x1[4], x1[5]), pack_rne(x1[6], x1[7])};
+    const uint32_t d2[4] = {pack_rne(x2[0], x2[1]), pack_rne(x2[2], x2[3]), pack_rne(x2[4], x2[5]), pack_rne(x2[6], x2[7])};
     if (h < q_heads) {
-      if (positions[t0 + t] < 0) continue;
+      if (position < 0) continue;
       uint16_t* q = q_out + ((t0 + t) * q_heads + h) * D + 8 * j;
       *reinterpret_cast<uint4*>(q) = make_uint4(d1[0], d1[1], d1[2], d1[3]);
       *reinterpret_cast<uint4*>(q + kHalf) = make_uint4(d2[0], d2[1], d2[2], d2[3]);
       continue;
     }
-    const int32_t slot = slots[t0 + t];
     if (slot < 0 || (uint64_t)slot >= size) continue;
     uint32_t c1[1], c2[1], p1, n1, p2, n2;
     cast_words_bf16<SCALE_KIND, ASYM, 8>(d1, 2, c1, p1, n1);
@@ -385,8 +422,8 @@ int amxfp4_paged_plan(const int32_t* lens, const int32_t* new_rows, int64_t seqs
     return report_error(AMX_ERR_INVALID_ARG, "paged_plan: pages and max_pages times page_size at most 2^30");
   if (lens_out == lens || state_out == state)
     return report_error(AMX_ERR_INVALID_ARG, "paged_plan: lens_out and state_out must be buffers of their own");
-  const int64_t blocks = (rows + 1023) / 1024;
-  hipLaunchKernelGGL(paged_plan_kernel, dim3((unsigned)(blocks < 1024 ? blocks : 1024)), dim3(256), 3 * sizeof(uint32_t) * (size_t)seqs,
+  const int64_t blocks = (rows + 255) / 256;
+  hipLaunchKernelGGL(paged_plan_kernel, dim3((unsigned)(blocks < 1024 ? blocks : 1024)), dim3(256), 4 * sizeof(uint32_t) * (size_t)seqs,
                      reinterpret_cast<hipStream_t>(stream), lens, new_rows, (int)seqs, (uint32_t)rows, l, (uint32_t)pages,
                      (uint32_t)max_pages, state, queue, table, lens_out, starts, slots, positions, state_out);
   return done("paged_plan launch");
@@ -403,11 +440,12 @@ int amxfp4_paged_write(const amx_format_t* fmt, const amx_paged_pool_t* pool, co
   if (!(theta > 1.0) || isinf(theta)) return report_error(AMX_ERR_INVALID_ARG, "paged_write: theta must exceed 1 and be finite");
   if (!aligned16(in) || ld % 4 || !aligned16(q_out_bf16) || !aligned4(slots) || !aligned4(positions))
     return report_error(AMX_ERR_INVALID_ARG, "paged_write: in and q_out must be 16-byte aligned, ld a multiple of 4");
-  const int64_t heads = q_heads + 2 * pool->kv_heads;
-  const dim3 grid((unsigned)((rows + kWriteRows - 1) / kWriteRows), (unsigned)((heads + kWriteHeads - 1) / kWriteHeads));
+  const int64_t heads = q_heads + 2 * pool->kv_heads, groups = (rows + kWriteRows - 1) / kWriteRows;
+  const int per_group = groups >= kWriteManyGroups ? (int)heads : (int)(256 / (pool->head_dim / 16 * kWriteRows));
+  const dim3 grid((unsigned)groups, (unsigned)((heads + per_group - 1) / per_group));
   for_pool(fmt, pool, [&]<int SK, bool ASYM, int D>() {
     hipLaunchKernelGGL((paged_write_kernel<SK, ASYM, D>), grid, dim3(256), 0, reinterpret_cast<hipStream_t>(stream), in, rows, ld,
-                       (int)q_heads, slots, positions, log(theta), static_cast<uint16_t*>(q_out_bf16), view(pool));
+                       (int)q_heads, slots, positions, log(theta), per_group, static_cast<uint16_t*>(q_out_bf16), view(pool));
   });
   return done("paged_write launch");
 }

@@ -66,7 +66,7 @@ struct PagedTail {
 
 // units of a worker: [first_unit(g), first_unit(g + 1))
 __device__ __forceinline__ uint32_t first_unit(uint32_t units, uint32_t groups, uint32_t g) {
-  return units / groups * g + (units % groups) * g / groups;  // (groups <= 3072)
+  return units / groups * g + (units % groups) * g / groups;  // (groups <= kMostWorkers)
 }
 
 template <int NC, int D>

@@ -71,6 +71,22 @@ def test_plan_of_nothing_and_of_everything_refused():
     check_plan([64, 16, 17], [-1, 1, 1], np.arange(12).reshape(3, 4), np.arange(8), [6, 1, 0, 0], 16, 2)
 
 
+def test_plan_after_a_refusal():
+    """What comes after a sequence that was refused for its pages: without a new page it is served, with one it is not; and rows
+    of long and short sequences that the batch's end cuts."""
+    table, queue = np.arange(20).reshape(5, 4) % 12, np.arange(12)
+    check_plan([14, 3, 30, 5, 16], [1, 40, 2, 3, 1], table, queue, [10, 2, 0, 0], 16, 60)
+    check_plan([16, 3, 30, 5, 16], [1, 40, 2, 9, 1], table, queue, [10, 2, 0, 0], 16, 60)
+    check_plan([16, 3, 30, 5, 16], [40, 1, 40, -1, 1], table, queue, [1, 0, 0, 0], 16, 90)
+    for rows in range(1, 40):
+        check_plan([5, 0, 16, 3, 7], [8, 9, 0, 12, 7], table, queue, [4, 12, 0, 0], 16, rows)
+    rng = np.random.RandomState(9)
+    for count in range(0, 9):
+        seqs = 700
+        lens, new = rng.randint(0, 40, seqs), rng.choice([0, 1, 1, 8, 9, -1], seqs, p=[.2, .3, .2, .1, .1, .1])
+        check_plan(lens, new, rng.permutation(seqs * 4).reshape(seqs, 4), np.arange(3000), [2995, 40 * count, 0, 0], 16, 1200)
+
+
 def test_plan_does_not_leave_its_buffers_whatever_they_hold():
     """Negative and huge lengths, ids outside the pool, a head and a count that are none: as if cut to the buffers."""
     rng = np.random.RandomState(1)
