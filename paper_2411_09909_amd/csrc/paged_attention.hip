@@ -715,8 +715,15 @@ int columns_of(int head_dim, int64_t rows, int64_t seqs, int64_t per) {
   return combinations <= 8 ? 2 : 1;
 }
 
-// Tokens up to which a sequence is not split over workgroups.
+// Tokens up to which a sequence is not split over workgroups: with 8 key heads, 64 sequences of up to 1000 tokens take 21 us whole and
+// 27 split, one of 700 10.4 and 11.9; one of 2000 20 whole and 12 split, 200 of them 105 and 86 (64 of them 39 and 43).
 bool is_whole(int64_t most_keys) { return most_keys <= 1024; }
+
+// Short sequences, and many for their length: a wave that has a sequence alone has nothing to share through LDS and to wait for, but the
+// longest takes four times as long as with four waves. 128 sequences with 8 key heads and up to 120, 300, 600 and 1000 tokens take 10, 16,
+// 25 and 37 us by the wave and 15, 19, 26 and 34 by four waves; 200 of up to 300, 500 and 600 23, 32 and 39 against 25, 29 and 34; 400 and
+// 1000 of up to 500 50 and 104 against 55 and 119; 64 of up to 120 8.3 and 8.5, of up to 600 24 and 17.
+bool is_by_wave(int64_t segments, int64_t most_keys) { return is_whole(most_keys) && 3 * segments >= 10 * most_keys; }
 
 }  // namespace
 
@@ -742,7 +749,7 @@ hipError_t launch_paged_attention(int scale_kind, bool asym, int head_dim, const
                        scale * 1.4426950408889634f, whole ? 1 : 0, unit_log2};
   const size_t values = 4 * kTile * (size_t)head_dim / 2, shares = 4 * (size_t)nc * head_dim * sizeof(float);
   const int64_t segments = seqs * pool.kv_heads;
-  const bool by_wave = whole && segments >= 1024;
+  const bool by_wave = is_by_wave(segments, most_keys);
   dim3 grid;
   int64_t workers = 0;
   size_t lds = by_wave || shares < values ? values : shares;

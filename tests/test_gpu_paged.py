@@ -316,6 +316,23 @@ def test_attention_most_sequences():
     check_attention(np.random.RandomState(5), "amxfp4_e4m3", 2, 1, 64, 16, lens, [int(b % 3 == 0) for b in range(4096)])
 
 
+@pytest.mark.parametrize("H,G,D,rows", [(16, 4, 128, 1), (32, 4, 128, 1), (64, 4, 128, 1), (12, 4, 128, 3), (16, 4, 64, 1), (64, 4, 64, 1)])
+def test_attention_short_sequences_by_the_wave(H, G, D, rows):
+    """More sequences and key heads than the card takes in workgroups, each for one wave: with every number of columns to a combination."""
+    rng = np.random.RandomState(H + D)
+    lens = list(rng.randint(1, 140, 258)) + [0, 280]
+    check_attention(rng, "amxfp4_e5m2", H, G, D, 32, lens, [min(rows, n) for n in lens], spare=1)
+
+
+@pytest.mark.parametrize("H,G,D,rows", [(8, 2, 128, 1), (4, 1, 64, 2), (16, 1, 128, 1)])
+def test_attention_split_with_more_sequences_than_are_kept(H, G, D, rows):
+    """Many sequences, most of them short, where the table has room for long ones."""
+    rng = np.random.RandomState(H + rows)
+    lens = list(rng.randint(0, 60, 700))
+    lens[3], lens[650] = 1300, 2100
+    check_attention(rng, "amxfp4_e5m2", H, G, D, 64, lens, [min(rows, n) for n in lens], width=34, spare=2)
+
+
 def test_attention_rows_that_see_nothing_and_pages_outside_the_pool():
     rng = np.random.RandomState(4)
     lens, rows = [70, 200, 16, 300], [2, 1, 2, 1]
