@@ -15,6 +15,8 @@ MLP width F:
 With fused_attention=True the two attention products and the softmax between them are one call (binding.attention):
 the attention map is not materialised and its tiles are cast relative to the running row maximum, which gives
 slightly different numbers than casting the normalised map.
+step() is the same layer for sequences that are being served: their new rows, packed into one batch, against the keys and values
+that a PagedCache holds. The queries and the probabilities stay BF16 there; keys and values are cast per token along D.
 """
 import math
 from dataclasses import dataclass
@@ -39,6 +41,33 @@ WEIGHT_SHAPES = lambda c: {  # noqa: E731  (name -> [out features, in features])
     "wq": (c.n_heads * c.head_dim, c.d_model), "wk": (c.n_kv_heads * c.head_dim, c.d_model),
     "wv": (c.n_kv_heads * c.head_dim, c.d_model), "wo": (c.d_model, c.n_heads * c.head_dim),
     "wg": (c.d_ff, c.d_model), "wu": (c.d_ff, c.d_model), "wd": (c.d_model, c.d_ff)}
+
+
+class PagedCache:
+    """The FP4 keys and values of up to `seqs` sequences for `layers` layers, in pages of `page_size` tokens that the sequences share
+    (a page has the same id in every layer), at most `max_keys` tokens to a sequence. All of it stays on the GPU: a step with plan()
+    and DecoderLayer.step() waits for nothing and can be captured in a graph."""
+
+    def __init__(self, cfg, fmt, seqs, pages, max_keys, page_size=64, layers=1, device="cuda"):
+        self.page_size = page_size
+        self.pools = [binding.paged_pool(fmt, pages, cfg.n_kv_heads, cfg.head_dim, page_size, device) for _ in range(layers)]
+        self.table = torch.full((seqs, -(-max_keys // page_size)), -1, dtype=torch.int32, device=device)
+        self.queue = torch.arange(pages, dtype=torch.int32, device=device)
+        # lengths | queue head, free pages, refused, rows: one buffer, so that a step moves them on with one copy
+        self._now = torch.zeros(seqs + 4, dtype=torch.int32, device=device)
+        self._now[seqs + 1] = pages
+        self.lens, self.state = self._now[:seqs], self._now[seqs:]
+
+    def plan(self, new_rows, rows):
+        """Pages and places for a step: new_rows int32 [seqs] on the GPU: how many of the batch's `rows` rows each sequence has, in its
+        order; -1 ends a sequence and gives its pages back, 0 leaves it alone. One call to a step, for all layers. A sequence whose rows
+        find no pages or no room is left as it was, and state[2] counts those: their rows have slot -1 and mean nothing behind step()."""
+        after = torch.empty_like(self._now)
+        out = (after[:self.lens.numel()], self.lens.new_empty(self.lens.numel() + 1), self.lens.new_empty(rows),
+               self.lens.new_empty(rows), after[self.lens.numel():])
+        plan = binding.paged_plan(self.lens, new_rows, self.table, self.queue, self.state, self.page_size, out=out)
+        self._now.copy_(after)
+        return plan
 
 
 class DecoderLayer:
@@ -75,15 +104,23 @@ class DecoderLayer:
             self.prepared = {id(w): binding.prepare_weights(fmt, w[0], w[1])
                              for w in (self.wqkv, self.wo, self.wgu, self.wd)}
 
+    def _workspace(self, need, device):
+        """One buffer that grows for the layer's calls, which run one after another; a graph gets buffers of its own, so that what it
+        was captured with neither goes away nor is another graph's too."""
+        if torch.cuda.is_current_stream_capturing():
+            return torch.empty(need, dtype=torch.uint8, device=device)
+        if self._ws is None or self._ws.numel() < need:
+            self._ws = torch.empty(need, dtype=torch.uint8, device=device)
+        return self._ws
+
     def _gemm(self, a, b):
         fmt = self.fmt
         batch = a[0].shape[0] if a[0].dim() == 3 else 1
         need = binding.gemm_workspace_bytes(fmt, a[0].shape[-2], b[0].shape[-2], a[0].shape[-1] * 2, batch)
-        if need and (self._ws is None or self._ws.numel() < need):
-            self._ws = torch.empty(need, dtype=torch.uint8, device=a[0].device)
+        ws = self._workspace(need, a[0].device) if need else None
         if self.prepared is not None and id(b) in self.prepared and batch == 1:
-            return binding.gemm_prepared(fmt, a[0], a[1], b[0], b[1], self.prepared[id(b)], workspace=self._ws)
-        return binding.gemm(fmt, a[0], a[1], b[0], b[1], workspace=self._ws if need else None, baseline=self.baseline)
+            return binding.gemm_prepared(fmt, a[0], a[1], b[0], b[1], self.prepared[id(b)], workspace=ws)
+        return binding.gemm(fmt, a[0], a[1], b[0], b[1], workspace=ws, baseline=self.baseline)
 
     def _plain_fmt(self):
         """the format for the entry points that have no mxfp4_* twin: symmetric when this layer is the baseline"""
@@ -98,10 +135,7 @@ class DecoderLayer:
         per = c.n_heads // G
         nsc = self.wqkv[1].shape[2:]  # () or (2,): scale entries per group
 
-        if self.fused_norm:
-            qkv = self._gemm(binding.rmsnorm_quantize(self._plain_fmt(), x, self.norm1, c.eps), self.wqkv)
-        else:
-            qkv = self._gemm(self._cast(binding.rmsnorm(x, self.norm1, c.eps)), self.wqkv)
+        qkv = self._qkv(x)
         v = binding.split_heads_rope(qkv, (c.n_heads + G) * D, G, D, False)
         if self.fused_rope:
             # rotary embedding and the cast of Q and K along the head dimension in one launch each (same bits)
@@ -116,12 +150,10 @@ class DecoderLayer:
             vc, vs = self._cast_v(v, nsc)
             fmt = binding.make_format(self.fmt.scale, False, 32) if self.baseline else self.fmt
             need = binding.attention_workspace_bytes(fmt, c.n_heads, G, S, S, D)
-            if self._ws is None or self._ws.numel() < need:
-                self._ws = torch.empty(need, dtype=torch.uint8, device=x.device)
             # (the kernel writes its output merged and in BF16: what merge_heads would make of the FP32 result)
             o = binding.attention(fmt, qc.view(c.n_heads, S, D // 2), qs.view(c.n_heads, S, D // 32, *nsc),
                                   kc.view(G, S, D // 2), ks.view(G, S, D // 32, *nsc), vc, vs, 1.0 / math.sqrt(D),
-                                  True, workspace=self._ws, merged=True)
+                                  True, workspace=self._workspace(need, x.device), merged=True)
             return self._after_attention(x, o)
         scores = self._gemm((qc.view(G, per * S, D // 2), qs.view(G, per * S, D // 32, *nsc)),
                             (kc.view(G, S, D // 2), ks.view(G, S, D // 32, *nsc)))
@@ -132,6 +164,23 @@ class DecoderLayer:
         vc, vs = self._cast_v(v, nsc)
         o = self._gemm((pc.view(G, per * S, S // 2), ps.view(G, per * S, S // 32, *nsc)), (vc, vs))
         return self._after_attention(x, binding.merge_heads(o, G, per, S, D))
+
+    def _qkv(self, x):
+        if self.fused_norm:
+            return self._gemm(binding.rmsnorm_quantize(self._plain_fmt(), x, self.norm1, self.cfg.eps), self.wqkv)
+        return self._gemm(self._cast(binding.rmsnorm(x, self.norm1, self.cfg.eps)), self.wqkv)
+
+    def step(self, x, cache, plan, layer=0, max_keys=0):
+        """x BF16 [rows, d_model]: the new rows of the cache's sequences, packed as in the `plan` that cache.plan() made for them (single
+        tokens, chunks of prompts or both). Stores their keys and values in pool `layer` of the cache, which is kept in the layer's
+        format (symmetric for the baseline), and returns the layer's output [rows, d_model]. Rows of refused sequences and behind the
+        last sequence come out without a meaning. max_keys: as for binding.paged_attention(). The layer's calls take turns on one stream, as in forward()."""
+        c = self.cfg
+        fmt, pool = self._plain_fmt(), cache.pools[layer]
+        q = binding.paged_write(fmt, self._qkv(x), pool, plan.slots, plan.positions, c.n_heads, c.rope_theta)
+        attn = binding.paged_attention(fmt, q, pool, cache.table, plan.lens, plan.starts, plan.positions, 1.0 / math.sqrt(c.head_dim),
+                                       max_keys=max_keys)
+        return self._after_attention(x, attn)
 
     def _cast_v(self, v, nsc):
         G, S, D = v.shape
@@ -153,9 +202,8 @@ class DecoderLayer:
         if self.fused_glu:
             fmt = self._plain_fmt()
             need = binding.gemm_silu_mul_workspace_bytes(fmt, hc[0].shape[0], c.d_ff, c.d_model)
-            if need and (self._ws is None or self._ws.numel() < need):
-                self._ws = torch.empty(need, dtype=torch.uint8, device=x.device)
-            act = binding.gemm_silu_mul(fmt, hc[0], hc[1], self.wgu[0], self.wgu[1], workspace=self._ws,
+            act = binding.gemm_silu_mul(fmt, hc[0], hc[1], self.wgu[0], self.wgu[1],
+                                        workspace=self._workspace(need, x.device) if need else None,
                                         prepared=self.prepared[id(self.wgu)] if self.prepared is not None else None)
         else:
             act = binding.silu_mul(self._gemm(hc, self.wgu))
