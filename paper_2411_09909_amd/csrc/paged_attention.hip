@@ -640,11 +640,11 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
 }
 
 // Adds up the partial results of one sequence, key head and tile of combinations: the second slot of the worker that began it, then
-// the first slots of those after it, in their order. One workgroup to a worker of the other kernel; most have nothing to do. A part's floats
-// are shared out over `kLanes` threads, the parts over the rest, eight requests of each under way at once.
-template <int D, int NC>
+// the first slots of those after it, in their order. SLICES workgroups to a worker of the other kernel; most have nothing to do. A part's
+// floats are shared out over the slices and `kLanes` threads, the parts over the rest, eight requests of each under way at once.
+template <int D, int NC, int SLICES>
 __global__ __launch_bounds__(512) void paged_attention_join_kernel(PagedWork w, uint32_t workers) {
-  constexpr int kLanes = NC * D / 4, kSets = 512 / kLanes;
+  constexpr int kLanes = NC * D / 4 / SLICES, kSets = 512 / kLanes;
   static_assert(kLanes <= 512, "one pass");
   const uint32_t g = blockIdx.x;
   const PagedTail t = reinterpret_cast<const PagedTail*>(w.workspace)[g];
@@ -659,7 +659,8 @@ __global__ __launch_bounds__(512) void paged_attention_join_kernel(PagedWork w, 
   auto part = [&](uint32_t i) { return parts + (2 * (size_t)(g + i) + (i == 0 ? 1 : 0)) * kPartFloats<NC, D>; };
   __shared__ float4 sums[kSets][kLanes];
   __shared__ float2 rest[kSets][kLanes];
-  const int set = threadIdx.x / kLanes, lane = threadIdx.x % kLanes, combo = lane / (D / 4), dim = 4 * (lane % (D / 4));
+  const int set = threadIdx.x / kLanes, lane = threadIdx.x % kLanes, at = (int)blockIdx.y * kLanes + lane;
+  const int combo = at / (D / 4), dim = 4 * (at % (D / 4));
   float4 sum = make_float4(0, 0, 0, 0);
   float total = 0.f, top = -INFINITY;
   // a set's parts, against their own running maximum
@@ -669,7 +670,7 @@ __global__ __launch_bounds__(512) void paged_attention_join_kernel(PagedWork w, 
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const float* p = part(min(i0 + k * kSets, count - 1));
-      v[k] = *reinterpret_cast<const float4*>(p + 4 * lane), m[k] = p[NC * D + combo], l[k] = p[NC * D + NC + combo];
+      v[k] = *reinterpret_cast<const float4*>(p + 4 * at), m[k] = p[NC * D + combo], l[k] = p[NC * D + NC + combo];
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -725,6 +726,13 @@ bool is_whole(int64_t most_keys) { return most_keys <= 1024; }
 // 1000 of up to 500 50 and 104 against 55 and 119; 64 of up to 120 8.3 and 8.5, of up to 600 24 and 17.
 bool is_by_wave(int64_t segments, int64_t most_keys) { return is_whole(most_keys) && 3 * segments >= 10 * most_keys; }
 
+// Workgroups that join the parts of a segment. With parts of 2048 floats one is left with a single set of threads, which takes them eight
+// at a time, one after another: up to 32 segments, of 24 parts and more, four of them do it sooner (16 rows and query heads to a key head, 4 key
+// heads: one sequence of 20000 tokens 31 -> 23 us, 4 of up to 30000 50 -> 44, 8 of up to 16000 54 -> 51); with more segments the workgroups
+// without work cost more (128 segments 52 -> 56), with smaller parts they do throughout (8 segments of 512 floats and 96 parts 52 -> 54).
+constexpr int join_slices(int floats) { return floats == 2048 ? 4 : 1; }
+constexpr int64_t kSlicedTiles = 64;  // (a bound that counts up to one tile too many to a sequence and key head)
+
 }  // namespace
 
 size_t paged_attention_workspace(int head_dim, int64_t rows, int64_t q_heads, int64_t kv_heads, int64_t seqs, int64_t) {
@@ -768,8 +776,12 @@ hipError_t launch_paged_attention(int scale_kind, bool asym, int head_dim, const
       hipLaunchKernelGGL((paged_attention_kernel<SK, ASYM, D, GC, 4>), grid, dim3(256), lds, s, pool, w, table, lens, starts, positions);
     else
       hipLaunchKernelGGL((paged_attention_kernel<SK, ASYM, D, GC, 1>), grid, dim3(256), lds, s, pool, w, table, lens, starts, positions);
-    if (!whole)
-      hipLaunchKernelGGL((paged_attention_join_kernel<D, 16 / GC>), dim3((unsigned)workers), dim3(512), 0, s, w, (uint32_t)workers);
+    if (whole) return hipGetLastError();
+    constexpr int kSlices = join_slices(16 / GC * D);
+    if (kSlices > 1 && tiles <= kSlicedTiles)
+      hipLaunchKernelGGL((paged_attention_join_kernel<D, 16 / GC, kSlices>), dim3((unsigned)workers, kSlices), dim3(512), 0, s, w, (uint32_t)workers);
+    else
+      hipLaunchKernelGGL((paged_attention_join_kernel<D, 16 / GC, 1>), dim3((unsigned)workers), dim3(512), 0, s, w, (uint32_t)workers);
     return hipGetLastError();
   };
   auto with_format = [&]<int SK, bool ASYM>() {

@@ -301,6 +301,12 @@ def test_attention_long_and_split(lens, rows, name, H, G, D, known):
     check_attention(rng, name, H, G, D, 64, lens, [min(rows, n) for n in lens], max_keys=max(lens) if known else 0)
 
 
+@pytest.mark.parametrize("lens,rows,H,G", [([9000], 1, 16, 1), ([3100, 1, 2000], 1, 32, 2), ([6000], 5, 8, 2), ([2000] * 20, 1, 64, 4)])
+def test_attention_long_with_all_columns_taken(lens, rows, H, G):
+    """Sixteen combinations to a tile: parts of 2048 floats, joined by several workgroups where there are few segments."""
+    check_attention(np.random.RandomState(H + rows), "amxfp4_e8m0", H, G, 128, 64, lens, [min(rows, n) for n in lens], spare=1)
+
+
 def test_attention_max_keys_too_small_costs_time_only():
     check_attention(np.random.RandomState(2), "amxfp4_e5m2", 8, 2, 128, 64, [3000, 40, 900], [1, 1, 2], max_keys=10)
 
