@@ -41,7 +41,10 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short i16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTile = 64;        // tokens of a unit
-constexpr int kMostWorkers = 768;  // of a launch that splits sequences: three workgroups to a compute unit, all at once
+// Workgroups of a launch that splits sequences, which are all to run at once: the registers leave room for three to a compute unit with four
+// columns to a combination and for two with two or one (and asymmetric scales). 16 sequences of 4 rows and 8 query heads to a key head 41 us on
+// 512 and 52 on 768; with heads of 64, where three or four have room, 512 are as good (8 sequences of up to 16000 tokens 21 and 22).
+constexpr int most_workers(int gc) { return gc == 4 ? 768 : 512; }
 // A sequence, key head and tile of combinations takes as long as this many tiles before its first one is in: the chain from the lengths
 // over the table to the keys, and the joining of the waves.
 constexpr uint32_t kStart = 12;
@@ -66,7 +69,7 @@ struct PagedTail {
 
 // units of a worker: [first_unit(g), first_unit(g + 1))
 __device__ __forceinline__ uint32_t first_unit(uint32_t units, uint32_t groups, uint32_t g) {
-  return units / groups * g + (units % groups) * g / groups;  // (groups <= kMostWorkers)
+  return units / groups * g + (units % groups) * g / groups;  // (groups <= 768)
 }
 
 template <int NC, int D>
@@ -737,7 +740,7 @@ constexpr int64_t kSlicedTiles = 64;  // (a bound that counts up to one tile too
 
 size_t paged_attention_workspace(int head_dim, int64_t rows, int64_t q_heads, int64_t kv_heads, int64_t seqs, int64_t) {
   // (whatever max_keys says: a sequence may be longer)
-  const int64_t nc = 16 / columns_of(head_dim, rows, seqs, q_heads / kv_heads), workers = kMostWorkers;
+  const int64_t nc = 16 / columns_of(head_dim, rows, seqs, q_heads / kv_heads), workers = most_workers(16 / (int)nc);
   return ((workers * sizeof(PagedTail) + 255) & ~(size_t)255) + 2 * workers * nc * (head_dim + 2) * sizeof(float);
 }
 
@@ -767,7 +770,7 @@ hipError_t launch_paged_attention(int scale_kind, bool asym, int head_dim, const
     grid = dim3((unsigned)(by_wave ? (segments + 3) / 4 : segments), (unsigned)(ct < 1024 ? ct : 1024));
   } else {
     const int64_t units = tiles * ((((most_keys + kTile - 1) / kTile) >> unit_log2) + 1 + kStart) / 4 + 1;
-    workers = units < kMostWorkers ? units : kMostWorkers;
+    workers = units < most_workers(gc) ? units : most_workers(gc);
     grid = dim3((unsigned)workers);
     lds += sequences_bytes(seqs);
   }
