@@ -13,7 +13,7 @@
  * launch, the return value is an amx_status_t, the message is available from amxfp4_last_error().
  * What lies on the device cannot be validated there. The calls never access memory outside the buffers that they are given,
  * whatever the lengths, tables, slots and queues say: a page id or slot outside the pool is not dereferenced, lengths and
- * row numbers are taken as if cut to what the buffers hold.
+ * row numbers are taken as if cut to what the buffers hold. Outputs and workspaces share no memory with anything else of a call.
  *
  * Layout of the pool, for each layer of a model its own (tables, slots and lengths are shared by the layers):
  *   codes    [pages][kv_heads][page_size][head_dim / 2] bytes, as amxfp4_quantize writes a row of head_dim elements;
@@ -112,7 +112,7 @@ int amxfp4_paged_read(const amx_format_t* fmt, const amx_paged_pool_t* pool, con
  * FP32 throughout, but the weights exp(s_j - running max), each times a scale of V, are rounded to BF16 for the matrix
  * instructions. A row that sees no key (position -1) gets zeros; rows behind the last sequence's are left as they were. Keys in
  * pages whose id lies outside the pool are not seen. Tokens from lens[b] on may hold anything, infinite scales too.
- *   q_bf16     [rows][q_heads][head_dim], 16-byte aligned, finite; out_bf16 [rows][q_heads * head_dim], 16-byte aligned.
+ *   q_bf16     [rows][q_heads][head_dim], 16-byte aligned, finite in rows that see a key; out_bf16 [rows][q_heads * head_dim], 16-byte aligned.
  *   table      [seqs][max_pages]; lens [seqs], starts [seqs + 1] (ascending), positions [rows]: as amxfp4_paged_plan wrote
  *              them (its lens_out).
  *   max_keys   at least the largest of lens, or 0 if not known (max_pages * page_size then). Work is divided by it; a sequence

@@ -712,7 +712,9 @@ __global__ __launch_bounds__(512) void paged_attention_join_kernel(PagedWork w, 
   *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16(all.x * inv, all.y * inv), pack_bf16(all.z * inv, all.w * inv));
 }
 
-// Columns to a combination: as many of the groups as leave room for the combinations that a sequence has on average.
+// Columns to a combination: as many of the groups as leave room for the combinations that a sequence has on average. (Fewer columns are less
+// work to a combination, but all combinations of a tile pay for it: 40 sequences of up to 3000 tokens with 8 query heads to a key head take
+// 40 us with two columns and 52 with four and two tiles; with 16 query heads 8 of up to 16000 41 us with one column and 51 with two.)
 int columns_of(int head_dim, int64_t rows, int64_t seqs, int64_t per) {
   const int64_t combinations = per * ((rows + seqs - 1) / seqs);
   if (head_dim == 128 && combinations <= 4) return 4;
@@ -731,7 +733,7 @@ bool is_by_wave(int64_t segments, int64_t most_keys) { return is_whole(most_keys
 
 // Workgroups that join the parts of a segment. With parts of 2048 floats one is left with a single set of threads, which takes them eight
 // at a time, one after another: up to 32 segments, of 24 parts and more, four of them do it sooner (16 rows and query heads to a key head, 4 key
-// heads: one sequence of 20000 tokens 31 -> 23 us, 4 of up to 30000 50 -> 44, 8 of up to 16000 54 -> 51); with more segments the workgroups
+// heads: one sequence of 20000 tokens 31 -> 23 us, 4 of up to 30000 34 -> 28, 8 of up to 16000 42 -> 41); with more segments the workgroups
 // without work cost more (128 segments 52 -> 56), with smaller parts they do throughout (8 segments of 512 floats and 96 parts 52 -> 54).
 constexpr int join_slices(int floats) { return floats == 2048 ? 4 : 1; }
 constexpr int64_t kSlicedTiles = 64;  // (a bound that counts up to one tile too many to a sequence and key head)

@@ -177,9 +177,13 @@ class DecoderLayer:
         last sequence come out without a meaning. max_keys: as for binding.paged_attention(). The layer's calls take turns on one stream, as in forward()."""
         c = self.cfg
         fmt, pool = self._plain_fmt(), cache.pools[layer]
-        q = binding.paged_write(fmt, self._qkv(x), pool, plan.slots, plan.positions, c.n_heads, c.rope_theta)
-        attn = binding.paged_attention(fmt, q, pool, cache.table, plan.lens, plan.starts, plan.positions, 1.0 / math.sqrt(c.head_dim),
-                                       max_keys=max_keys)
+        rows = x.shape[0]
+        q = torch.empty((rows, c.n_heads, c.head_dim), dtype=torch.bfloat16, device=x.device)
+        binding.paged_write(fmt, self._qkv(x), pool, plan.slots, plan.positions, c.n_heads, c.rope_theta, q=q)
+        need = binding.paged_attention_workspace_bytes(fmt, pool, rows, c.n_heads, cache.lens.numel(), max_keys)
+        attn = torch.empty((rows, c.n_heads * c.head_dim), dtype=torch.bfloat16, device=x.device)
+        binding.paged_attention(fmt, q, pool, cache.table, plan.lens, plan.starts, plan.positions, 1.0 / math.sqrt(c.head_dim), max_keys,
+                                out=attn, workspace=self._workspace(need, x.device))
         return self._after_attention(x, attn)
 
     def _cast_v(self, v, nsc):

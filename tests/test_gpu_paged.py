@@ -353,6 +353,21 @@ def test_attention_rows_that_see_nothing_and_pages_outside_the_pool():
     assert (out[[0, 2, 3, 4]] == 0).all() and (out[1] != 0).any()
 
 
+@pytest.mark.parametrize("H,G,D", [(8, 2, 128), (32, 2, 128), (8, 8, 64)])
+@pytest.mark.parametrize("width", [10, 80])
+def test_attention_queries_of_rows_that_see_nothing_may_hold_anything(H, G, D, width):
+    """Rows that were refused keep what their memory held: NaN and infinities there reach no other row and give zeros."""
+    rng = np.random.RandomState(H)
+    lens, rows = [70, 200, 0, 300], [3, 2, 1, 1]
+    fmt, pool, table = filled(rng, "amxfp4_e5m2", G, D, 32, lens, width)
+    starts, positions = np.concatenate([[0], np.cumsum(rows)]), np.array([-1, 68, -1, 198, -1, -1, 299])
+    q = torch.from_numpy(rng.randn(7, H, D).astype(np.float32)).to(torch.bfloat16).cuda()
+    spoiled = q.clone()
+    spoiled[torch.from_numpy(positions < 0)] = torch.tensor([float("nan"), float("inf"), -float("inf"), 3e38] * (D // 4)).to(torch.bfloat16).cuda()
+    a, b = (binding.paged_attention(fmt, x, pool, dev(table), dev(lens), dev(starts), dev(positions), 0.1) for x in (q, spoiled))
+    assert torch.equal(a, b) and (a[torch.from_numpy(positions < 0)] == 0).all() and (a[torch.from_numpy(positions >= 0)] != 0).any(1).all()
+
+
 def test_attention_beyond_four_gigabytes():
     """Codes at byte offsets over 2^32: the pages at the end of a large pool."""
     rng = np.random.RandomState(6)
