@@ -24,6 +24,12 @@
 //            range from the lengths (a prefix sum over the sequences, in LDS). A range may begin and end within a sequence: those
 //            partial results (O, m, l) go to the workspace, at most two to a workgroup, and paged_attention_join_kernel adds them up.
 //   whole    short sequences: a sequence and key head to a workgroup or, where there are many, to a wave, with all its tokens.
+//
+// Bound and measured (both kernels, back to back). 64 sequences of up to 16384 tokens, 32 / 8 heads of 128, pairs of E5M2 scales, 612 MB:
+// 133 us = 4.6 TB/s; pieces of 4 KB from all over the memory are read at 5.9 TB/s by loads alone (104 us), and the vector instructions
+// (conversion, scales, softmax: some 2400 cycles a tile and SIMD) hide in that but for their unevenness. One of 131000 tokens, 151 MB: 48 us,
+// of which 7 are the join. 16 of up to 4000 with 4 rows of 8 query heads to a key head, 42 MB: 39 us, bound by the vector instructions. One of 700: 10 us,
+// the chain from the lengths to the codes and the waves' join.
 #include "paged.h"
 
 #include "kernels.h"
