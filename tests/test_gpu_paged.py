@@ -164,6 +164,26 @@ def test_rows_written_as_the_oracle_and_the_separate_calls_have_them(name, H, G,
     assert torch.equal(q[t], binding.split_heads_rope(xs, 0, H, D, True, int(positions[t]), THETA)[:, 0])
 
 
+@pytest.mark.parametrize("H,G,D,rows", [(3, 1, 64, 2051), (9, 2, 128, 2046), (1024, 1, 64, 3), (5, 1024, 64, 2)])
+def test_rows_written_many_rows_and_many_heads(H, G, D, rows):
+    """Long prompts, where a workgroup has all heads of its rows; and the most heads."""
+    rng = np.random.RandomState(rows)
+    kind, asym = FORMATS["amxfp4_e5m2"]
+    fmt, pages, page = binding.make_format(kind, asym), -(-rows // 64) + 2, 64
+    x = activations(rng, rows, (H + 2 * G) * D + 4)
+    slots, positions = rng.permutation(pages * page)[:rows].astype(np.int32), rng.randint(0, 3 * 10 ** 5, rows).astype(np.int32)
+    slots[rows // 2], positions[rows // 2] = -1, -1
+    pool = make_pool(fmt, pages, G, D, page)
+    want = host_pool(pool)
+    q = torch.full((rows, H, D), 3.0, dtype=torch.bfloat16, device="cuda")
+    binding.paged_write(fmt, torch.from_numpy(x).cuda(), pool, dev(slots), dev(positions), H, THETA, q=q)
+    want_q = paged_ref.write(x, want, slots, positions, H, THETA, kind, asym)
+    want_q[positions < 0] = 0x4040
+    np.testing.assert_array_equal(bits(q).reshape(rows, H, D), want_q)
+    for n, t in zip(NAMES, pool):
+        np.testing.assert_array_equal(t.cpu().numpy(), want[n], err_msg=n)
+
+
 @pytest.mark.parametrize("name", FORMATS)
 @pytest.mark.parametrize("G,D,page,rows", [(2, 128, 16, 1), (12, 64, 32, 50), (1, 64, 256, 7), (8, 128, 64, 333)])
 def test_rows_read_back(name, G, D, page, rows):
@@ -305,6 +325,14 @@ def test_attention_long_and_split(lens, rows, name, H, G, D, known):
 def test_attention_long_with_all_columns_taken(lens, rows, H, G):
     """Sixteen combinations to a tile: parts of 2048 floats, joined by several workgroups where there are few segments."""
     check_attention(np.random.RandomState(H + rows), "amxfp4_e8m0", H, G, 128, 64, lens, [min(rows, n) for n in lens], spare=1)
+
+
+@pytest.mark.parametrize("lens,rows,H,G,D,width", [
+    ([2100, 5], [2000, 1], 4, 2, 64, 34), ([900, 0, 77], [900, 0, 77], 2, 1, 128, 15),   # chunks of prompts
+    ([40, 3, 17], [1, 1, 1], 1024, 1, 64, 1), ([70, 3], [1, 2], 1024, 1024, 64, 2), ([1100], [1], 1024, 2, 128, 20),   # the most heads
+    ([1 + b % 70 for b in range(4096)], [int(b % 2 == 0) for b in range(4096)], 1, 1, 64, 18)])   # the most sequences, split
+def test_attention_at_the_limits(lens, rows, H, G, D, width):
+    check_attention(np.random.RandomState(H + D), "amxfp4_e5m2", H, G, D, 64, lens, rows, width=width)
 
 
 def test_attention_max_keys_too_small_costs_time_only():
