@@ -6,14 +6,14 @@
 // group g of the keys alone (the query's other groups are zeros there), so that the group's scales, which are those of a token,
 // can be applied to the product: s[c][j] = sum_g S[j][g] (q . elements)[c][j][g]. The keys' elements are converted to BF16, which
 // holds them, and not scaled.
-//   sign pair   S_p q.e+ + S_n q.e- = S_n q.e + (S_p - S_n) q.e+: two products, in FP32; what cancels is 2^-23 of the larger
-//               scale's share.
+//   sign pair   S_p q.e+ + S_n q.e-: a product to each sign class. (S_n q.e + (S_p - S_n) q.e+ would save separating e-, but where S_n is much the
+//               larger the positive class is the difference of two terms of its size: with S_n / S_p = 2^16 and a query of zeros on the negative
+//               elements' dimensions a score was off by 2^-10 of sum |q k|, with 2^28 it was lost.)
 //   (The codes as they are on the block-scaled instruction, the query as two E4M3 parts, saves the conversion and costs
 //   exactness: that instruction adds its products in a window of 2^-13 of the largest, and a score was off by 2^-12 of it.)
 // Values. The codes of 64 tokens are transposed by ds_read_b64_tr_b4 (16 lanes read 16 rows of 16 codes and get one column
 // each), converted to BF16 elements and multiplied with p[c][j] S[j][g], rounded to BF16: O[d][c] = sum_j (p S)[j][c] e[j][d].
-// The two sign classes stay apart here (e+ with p S_p, e- with p S_n): with p S_n and p (S_p - S_n) the rounding of a much
-// larger S_n would drown the positive class. The columns of the other groups compute products nobody reads.
+// The two sign classes stay apart here too (e+ with p S_p, e- with p S_n). The columns of the other groups compute products nobody reads.
 // Layout of a tile of 64 tokens in a wave: lane (column or row r = l % 16, quarter u = l / 16). S^T comes out of the matrix
 // instruction t (of 4) with tile rows 4 u + i in lane (r, u): those rows are keys 16 u + 4 t + i, so that a lane holds the 16 keys
 // 16 u .. of its column, in the order in which the second product wants them, and needs the scales of 16 neighbouring tokens, 32 bytes.
@@ -433,13 +433,13 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
         for (int i = 0; i < 4; ++i) x[4 * t + i] = 0.f;
 #pragma unroll
         for (int st = 0; st < GS; ++st) {
-          f32x4 dot = {0, 0, 0, 0}, with = {0, 0, 0, 0};
+          f32x4 dot = {0, 0, 0, 0}, negatives = {0, 0, 0, 0};  // (both signs, where they have one scale; the positive class else)
 #pragma unroll
           for (int j = st * GC; j < (st + 1) * GC; ++j) {
             const u32x4 e = elements(kw[Tile::kGroups * t + j]);  // (heads of 64: two tiles' words in turn)
             const bf16x8 qj = __builtin_bit_cast(bf16x8, q[j]);
-            dot = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, e), qj, dot, 0, 0, 0);
-            if constexpr (ASYM) with = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, positive(e)), qj, with, 0, 0, 0);
+            dot = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ASYM ? positive(e) : e), qj, dot, 0, 0, 0);
+            if constexpr (ASYM) negatives = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, negative(e)), qj, negatives, 0, 0, 0);
           }
           if constexpr (ASYM) {
             const uint32_t s0 = d.ks[st][t >> 1][2 * t & 3], s1 = d.ks[st][t >> 1][(2 * t + 1) & 3];
@@ -447,7 +447,7 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
                                 two_scales<SCALE_KIND, true>(s1)};
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              x[4 * t + i] = __builtin_fmaf(a[i][1], dot[i], __builtin_fmaf(a[i][0] - a[i][1], with[i], x[4 * t + i]));
+              x[4 * t + i] = __builtin_fmaf(a[i][1], negatives[i], __builtin_fmaf(a[i][0], dot[i], x[4 * t + i]));
           } else {
             const uint32_t s0 = d.ks[st][0][t];
             const f32x2 a = two_scales<SCALE_KIND, false>(s0), z = two_scales<SCALE_KIND, true>(s0);
