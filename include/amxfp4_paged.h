@@ -114,7 +114,7 @@ int amxfp4_paged_read(const amx_format_t* fmt, const amx_paged_pool_t* pool, con
  * pages whose id lies outside the pool are not seen. Tokens from lens[b] on may hold anything, infinite scales too.
  *   q_bf16     [rows][q_heads][head_dim], 16-byte aligned, finite in rows that see a key; out_bf16 [rows][q_heads * head_dim], 16-byte aligned.
  *   table      [seqs][max_pages]; lens [seqs], starts [seqs + 1] (ascending), positions [rows]: as amxfp4_paged_plan wrote
- *              them (its lens_out).
+ *              them (its lens_out). A position from lens[b] on, up to 2^31 - 1, sees all that the sequence holds.
  *   max_keys   at least the largest of lens, or 0 if not known (max_pages * page_size then). Work is divided by it; a sequence
  *              that is longer all the same costs time only.
  *   workspace  at least amxfp4_paged_attention_workspace_bytes() bytes, 256-byte aligned (AMX_ERR_WORKSPACE otherwise); partial

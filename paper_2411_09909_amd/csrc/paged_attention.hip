@@ -384,7 +384,8 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
     look_up(tile + SHARE);
 
     // tokens it sees; columns that nobody asked for see all and are not looked at
-    const int limit = asked ? min(max(position, -1) + 1, (int)s.keys) : 0x7FFFFFFF;
+    // (positions may be the type's ends: one is added only below the keys' number)
+    const int limit = asked ? min(max(position, -1), (int)s.keys - 1) + 1 : 0x7FFFFFFF;
     int least = limit, most = asked ? limit : 0;  // (the same in all quarters and in the columns of a combination)
 #pragma unroll
     for (int o = GC; o < 16; o <<= 1) least = min(least, __shfl_xor(least, o, 64)), most = max(most, __shfl_xor(most, o, 64));
