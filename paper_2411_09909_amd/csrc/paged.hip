@@ -461,13 +461,19 @@ int amxfp4_paged_read(const amx_format_t* fmt, const amx_paged_pool_t* pool, con
     return report_error(AMX_ERR_INVALID_ARG, "paged_read: outputs must be 16-byte aligned");
   for_pool(fmt, pool, [&]<int SK, bool ASYM, int D>() {
     constexpr int kFormat = SK == kScaleE8M0Round ? kScaleE8M0Floor : SK;  // one encoding of the bytes
-    const dim3 grid((unsigned)((rows * pool->kv_heads * (D / 8) + 255) / 256), 2);
-    if (out_dtype == 1)
-      hipLaunchKernelGGL((paged_read_kernel<kFormat, ASYM, D, true>), grid, dim3(256), 0, reinterpret_cast<hipStream_t>(stream), slots,
-                         rows, view(pool), k_out, v_out);
-    else
-      hipLaunchKernelGGL((paged_read_kernel<kFormat, ASYM, D, false>), grid, dim3(256), 0, reinterpret_cast<hipStream_t>(stream), slots,
-                         rows, view(pool), k_out, v_out);
+    // (a launch has fewer than 2^32 threads: rows at a time, all of them but where the outputs take 64 GB)
+    const int64_t row_items = (int64_t)pool->kv_heads * (D / 8), most = (int64_t(1) << 31) / row_items;
+    for (int64_t r = 0; r < rows; r += most) {
+      const int64_t n = rows - r < most ? rows - r : most, at = r * row_items * 8 * (out_dtype == 1 ? 2 : 4);
+      const dim3 grid((unsigned)((n * row_items + 255) / 256), 2);
+      void *k = static_cast<uint8_t*>(k_out) + at, *v = static_cast<uint8_t*>(v_out) + at;
+      if (out_dtype == 1)
+        hipLaunchKernelGGL((paged_read_kernel<kFormat, ASYM, D, true>), grid, dim3(256), 0, reinterpret_cast<hipStream_t>(stream),
+                           slots + r, n, view(pool), k, v);
+      else
+        hipLaunchKernelGGL((paged_read_kernel<kFormat, ASYM, D, false>), grid, dim3(256), 0, reinterpret_cast<hipStream_t>(stream),
+                           slots + r, n, view(pool), k, v);
+    }
   });
   return done("paged_read launch");
 }
