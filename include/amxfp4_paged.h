@@ -120,7 +120,7 @@ int amxfp4_paged_read(const amx_format_t* fmt, const amx_paged_pool_t* pool, con
  *   workspace  at least amxfp4_paged_attention_workspace_bytes() bytes, 256-byte aligned (AMX_ERR_WORKSPACE otherwise); partial
  *              results of this call alone: calls that may run at the same time need one each.
  *   limits     group_size 32; q_heads a multiple of kv_heads, at most 1024; rows <= 2^24, rows * q_heads <= 2^31; seqs <= 4096;
- *              max_pages * page_size <= 2^30; scale > 0.
+ *              max_pages * page_size <= 2^30; 0 < scale <= 2^127.
  * The split of the work, and with it the order of the FP32 sums, depends on all sequences of the call: a sequence's result
  * is not bit for bit the same in another batch. The same call gives the same bits.
  */

@@ -498,7 +498,8 @@ int amxfp4_paged_attention(const amx_format_t* fmt, const amx_paged_pool_t* pool
       seqs > kPagedMaxSeqs || max_pages <= 0 || max_pages > kMaxTokens / pool->page_size || max_keys < 0 || max_keys > kMaxTokens ||
       rows * q_heads > kMaxQueries)
     return report_error(AMX_ERR_INVALID_ARG, "paged_attention: bad shape (q_heads a multiple of kv_heads, 1 to 4096 sequences)");
-  if (!(scale > 0.f) || isinf(scale)) return report_error(AMX_ERR_INVALID_ARG, "paged_attention: scale must be positive and finite");
+  // (the kernel's scale is this times log2 e, which has to be finite too)
+  if (!(scale > 0.f) || scale > 0x1p127f) return report_error(AMX_ERR_INVALID_ARG, "paged_attention: scale must be positive, at most 2^127");
   if (!aligned16(q_bf16) || !aligned16(out_bf16) || !aligned4(table) || !aligned4(lens) || !aligned4(starts) || !aligned4(positions))
     return report_error(AMX_ERR_INVALID_ARG, "paged_attention: q and out must be 16-byte aligned");
   const size_t need = paged_attention_workspace(pool->head_dim, rows, q_heads, pool->kv_heads, seqs, max_keys);
