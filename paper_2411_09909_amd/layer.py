@@ -178,6 +178,9 @@ class DecoderLayer:
         c = self.cfg
         fmt, pool = self._plain_fmt(), cache.pools[layer]
         rows = x.shape[0]
+        if pool.k_codes.shape[1] != c.n_kv_heads or pool.k_codes.shape[3] * 2 != c.head_dim:  # (a narrower one would take the wrong columns)
+            raise binding.AmxError("step: a cache of %d key heads of %d, the layer has %d of %d" % (
+                pool.k_codes.shape[1], pool.k_codes.shape[3] * 2, c.n_kv_heads, c.head_dim))
         q = torch.empty((rows, c.n_heads, c.head_dim), dtype=torch.bfloat16, device=x.device)
         binding.paged_write(fmt, self._qkv(x), pool, plan.slots, plan.positions, c.n_heads, c.rope_theta, q=q)
         need = binding.paged_attention_workspace_bytes(fmt, pool, rows, c.n_heads, cache.lens.numel(), max_keys)
