@@ -73,6 +73,11 @@ size_t amxfp4_paged_scales_bytes(const amx_format_t* fmt, const amx_paged_pool_t
  * The outputs are buffers of their own: lens_out must not be lens, state_out not state (AMX_ERR_INVALID_ARG): the call has no
  * order between reading and writing them. The same inputs give the same outputs and entries, so that a call may be repeated.
  * A program keeps two sets of lens and state and uses them in turn.
+ * A sequence grows or ends, it does not shrink: lens are 0 or what an earlier call wrote. Behind a length that the caller lowers, pages
+ * are lost: the sequence takes new ones for tokens whose pages it had, and gives back only those that the lower length counts.
+ * Rows that turn out not to be wanted (of a draft) are taken back by planning the step again: as nothing that the call reads has
+ * changed, the same lens, state, queue and table with the numbers of accepted rows give what they would have given without the
+ * draft. Pages may be others then, so that the accepted rows are written again, at the second plan's slots.
  *   limits    seqs <= 4096; rows <= 2^30; max_pages * page_size <= 2^30; pages * page_size <= 2^30; page_size as in the pool.
  */
 int amxfp4_paged_plan(const int32_t* lens, const int32_t* new_rows, int64_t seqs, int64_t rows, int64_t page_size,
@@ -110,8 +115,9 @@ int amxfp4_paged_read(const amx_format_t* fmt, const amx_paged_pool_t* pool, con
  *     s_j = scale * sum_d q[t][h][d] K_hat[j][d]          for tokens j <= positions[t], j < lens[b]
  *     out[t][h][:] = bf16( sum_j exp(s_j - max s) V_hat[j][:] / sum_j exp(s_j - max s) )
  * FP32 throughout, but the weights exp(s_j - running max), each times a scale of V, are rounded to BF16 for the matrix
- * instructions. A row that sees no key (position -1) gets zeros; rows behind the last sequence's are left as they were. Keys in
- * pages whose id lies outside the pool are not seen. Tokens from lens[b] on may hold anything, infinite scales too.
+ * instructions; sums that leave FP32's range (of exp(s_j - max) |V_hat| too, before the division) are infinite. A row that sees no key (position -1) gets zeros; rows behind the last sequence's are left as they were. Keys in
+ * pages whose id lies outside the pool are not seen. Tokens from lens[b] on may hold anything, infinite scales too. The
+ * least power-of-two scale (byte 0, 2^-127) counts as 0.
  *   q_bf16     [rows][q_heads][head_dim], 16-byte aligned, finite in rows that see a key; out_bf16 [rows][q_heads * head_dim], 16-byte aligned.
  *   table      [seqs][max_pages]; lens [seqs], starts [seqs + 1] (ascending), positions [rows]: as amxfp4_paged_plan wrote
  *              them (its lens_out). A position from lens[b] on, up to 2^31 - 1, sees all that the sequence holds.

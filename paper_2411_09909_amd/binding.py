@@ -732,7 +732,8 @@ def paged_pool(fmt, pages, kv_heads, head_dim, page_size, device="cuda"):
 def paged_plan(lens, new_rows, table, queue, state, page_size, rows=None, out=None):
     """amxfp4_paged_plan: pages, slots and positions for one step. lens, new_rows int32 [seqs]; table int32 [seqs, max_pages] and
     queue int32 [pages], updated in place; state int32 [4], left alone. rows: how many the packed batch has room for (default:
-    those of `out`, buffers as in PagedPlan). Returns a PagedPlan: its lens and state are the next step's."""
+    those of `out`, buffers as in PagedPlan). Returns a PagedPlan: its lens and state are the next step's. Sequences do not shrink: to take
+    rows back, plan the step again from the same lens and state, with fewer, and write those again."""
     if out is not None and rows is None:
         rc = (_calls or _bound()).paged_plan(lens, new_rows, table, queue, state, page_size, out)
         if rc is not None:

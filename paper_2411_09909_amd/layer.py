@@ -45,7 +45,7 @@ WEIGHT_SHAPES = lambda c: {  # noqa: E731  (name -> [out features, in features])
 
 class PagedCache:
     """The FP4 keys and values of up to `seqs` sequences for `layers` layers, in pages of `page_size` tokens that the sequences share
-    (a page has the same id in every layer), at most `max_keys` tokens to a sequence. All of it stays on the GPU: a step with plan()
+    (a page has the same id in every layer), at most `max_keys` tokens, rounded up to whole pages, to a sequence. All of it stays on the GPU: a step with plan()
     and DecoderLayer.step() waits for nothing and can be captured in a graph."""
 
     def __init__(self, cfg, fmt, seqs, pages, max_keys, page_size=64, layers=1, device="cuda"):
@@ -61,7 +61,9 @@ class PagedCache:
     def plan(self, new_rows, rows):
         """Pages and places for a step: new_rows int32 [seqs] on the GPU: how many of the batch's `rows` rows each sequence has, in its
         order; -1 ends a sequence and gives its pages back, 0 leaves it alone. One call to a step, for all layers. A sequence whose rows
-        find no pages or no room is left as it was, and state[2] counts those: their rows have slot -1 and mean nothing behind step()."""
+        find no pages or no room is left as it was, and state[2] counts those: their rows have slot -1 and mean nothing behind step().
+        A sequence does not shrink. To take back rows of a draft, keep copies of `lens` and `state` from before its plan, copy them back, and
+        plan and store the accepted rows as if there had been no draft (they may come into other pages)."""
         after = torch.empty_like(self._now)
         out = (after[:self.lens.numel()], self.lens.new_empty(self.lens.numel() + 1), self.lens.new_empty(rows),
                self.lens.new_empty(rows), after[self.lens.numel():])
