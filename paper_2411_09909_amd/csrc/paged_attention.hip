@@ -25,11 +25,12 @@
 //            partial results (O, m, l) go to the workspace, at most two to a workgroup, and paged_attention_join_kernel adds them up.
 //   whole    short sequences: a sequence and key head to a workgroup or, where there are many, to a wave, with all its tokens.
 //
-// Bound and measured (both kernels, back to back). 64 sequences of up to 16384 tokens, 32 / 8 heads of 128, pairs of E5M2 scales, 612 MB:
-// 133 us = 4.6 TB/s; pieces of 4 KB from all over the memory are read at 5.9 TB/s by loads alone (104 us), and the vector instructions
-// (conversion, scales, softmax: some 2400 cycles a tile and SIMD) hide in that but for their unevenness. One of 131000 tokens, 151 MB: 48 us,
-// of which 7 are the join. 16 of up to 4000 with 4 rows of 8 query heads to a key head, 42 MB: 39 us, bound by the vector instructions. One of 700: 10 us,
-// the chain from the lengths to the codes and the waves' join.
+// Bound and measured (a pass of both kernels, back to back; medians; cards differ by some 4 %). 64 sequences of up to 16384 tokens, 32 / 8 heads of
+// 128, pairs of E5M2 scales, 612 MB: 145 us = 4.2 TB/s (140 before the scores kept the sign classes apart); pieces of 4 KB from all over the memory
+// are read at 5.9 TB/s by loads alone (104 us), and the vector instructions (conversion, scales, softmax: 787 to a tile and wave) hide in that but
+// for their unevenness. One of 131000 tokens, 151 MB: 49 us, of which 7 to 10 are the join. 16 of up to 4000 with up to 4 rows of 8 query heads to a
+// key head, 42 MB: 39 us, bound by the vector instructions. One of 700: 10 us, the chain from the lengths to the codes and the waves' join.
+// Not dealt out evenly are sequences taken whole (tables, or max_keys, of up to 1024 tokens) of which a few have many rows: see is_whole().
 #include "paged.h"
 
 #include "kernels.h"
@@ -48,8 +49,10 @@ typedef short i16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTile = 64;        // tokens of a unit
 // Workgroups of a launch that splits sequences, which are all to run at once: the registers leave room for three to a compute unit with four
-// columns to a combination and for two with two or one (and asymmetric scales). 16 sequences of 4 rows and 8 query heads to a key head 41 us on
-// 512 and 52 on 768; with heads of 64, where three or four have room, 512 are as good (8 sequences of up to 16000 tokens 21 and 22).
+// columns to a combination and for two with two or one and asymmetric scales. 16 sequences of 4 rows and 8 query heads to a key head 41 us on
+// 512 and 52 on 768, 40 of up to 3000 tokens with 8 query heads to a key head 41 and 48. Where three or four have room with fewer columns, 512 are as
+// good: symmetric scales and two columns, the same 40 sequences 31.2 us and 31.7, 16 of up to 8000 28.1 and 26.8, 4 of up to 30000 27.0 and 27.6;
+// heads of 64, 8 sequences of up to 16000 tokens 21 and 22.
 constexpr int most_workers(int gc) { return gc == 4 ? 768 : 512; }
 // A sequence, key head and tile of combinations takes as long as this many tiles before its first one is in: the chain from the lengths
 // over the table to the keys, and the joining of the waves.
@@ -730,6 +733,8 @@ int columns_of(int head_dim, int64_t rows, int64_t seqs, int64_t per) {
 
 // Tokens up to which a sequence is not split over workgroups: with 8 key heads, 64 sequences of up to 1000 tokens take 21 us whole and
 // 27 split, one of 700 10.4 and 11.9; one of 2000 20 whole and 12 split, 200 of them 105 and 86 (64 of them 39 and 43).
+// All measured with as many rows to each sequence. A sequence with many rows among others with few has its tiles of combinations one after
+// another, in as many workgroups to a key head as the sequences need on average (the launch's y), where splitting would deal them out.
 bool is_whole(int64_t most_keys) { return most_keys <= 1024; }
 
 // Short sequences, and many for their length: a wave that has a sequence alone has nothing to share through LDS and to wait for, but the
