@@ -102,9 +102,9 @@ int amxfp4_paged_write(const amx_format_t* fmt, const amx_paged_pool_t* pool, co
                        void* stream);
 
 /*
- * What the cache holds at `rows` slots, dequantized (Eq. 1; exact in both types, but 2^128, which a rounded power-of-two scale can give, is
- * infinite): k_out, v_out [rows][kv_heads][head_dim],
- * 16-byte aligned, out_dtype 0 = float32, 1 = BF16 bit patterns. A slot outside the pool gives a row of zeros. rows <= 2^24.
+ * What the cache holds at `rows` slots, dequantized (Eq. 1; exact in both types, but 2^128, which a rounded power-of-two scale can give,
+ * is infinite): k_out, v_out [rows][kv_heads][head_dim], 16-byte aligned, out_dtype 0 = float32, 1 = BF16 bit patterns. A slot outside
+ * the pool gives a row of zeros. rows <= 2^24.
  */
 int amxfp4_paged_read(const amx_format_t* fmt, const amx_paged_pool_t* pool, const int32_t* slots, int64_t rows,
                       int32_t out_dtype, void* k_out, void* v_out, void* stream);

@@ -461,7 +461,7 @@ int amxfp4_paged_read(const amx_format_t* fmt, const amx_paged_pool_t* pool, con
     return report_error(AMX_ERR_INVALID_ARG, "paged_read: outputs must be 16-byte aligned");
   for_pool(fmt, pool, [&]<int SK, bool ASYM, int D>() {
     constexpr int kFormat = SK == kScaleE8M0Round ? kScaleE8M0Floor : SK;  // one encoding of the bytes
-    // (a launch has fewer than 2^32 threads: rows at a time, all of them but where the outputs take 64 GB)
+    // (a launch has fewer than 2^32 threads: rows at a time, which are all of them up to 2^34 elements of K)
     const int64_t row_items = (int64_t)pool->kv_heads * (D / 8), most = (int64_t(1) << 31) / row_items;
     for (int64_t r = 0; r < rows; r += most) {
       const int64_t n = rows - r < most ? rows - r : most, at = r * row_items * 8 * (out_dtype == 1 ? 2 : 4);
