@@ -189,7 +189,7 @@ def _prepare_prompt(s, gen):
     for name, heads, rows, shift in (("q", H, Sq, 0.3), ("k", G, Sk, 0.5), ("v", G, Sk, 1.0)):
         x = _values(gen, heads * rows, D, shift).view(heads, rows, D)
         codes, scales = _cast(x.transpose(1, 2) if name == "v" else x, kind, asym)
-        s[name] = _packed(codes), scales.contiguous()
+        s[name] = _packed(codes).contiguous(), scales.contiguous()
     if case["mask"] == "causal":
         s["first"] = s["last"] = None
     else:
@@ -238,8 +238,8 @@ def _prepare_tokens(s, gen):
     s["logits"].normal_(0.0, 2.5, generator=gen)
     if case["ld"] > V:
         wide[:, V:] = math.nan  # not part of a row
-    # a few candidates stand out in every row; half of the tokens are among them
-    at = torch.randint(0, V, (T, 24), generator=gen, device=DEV)
+    # a few candidates, each another token, stand out in every row; half of the targets are among them
+    at = (torch.randint(0, V, (T, 1), generator=gen, device=DEV) + torch.arange(24, device=DEV) * (V // 24)) % V
     up = torch.rand((T, 24), generator=gen, device=DEV) * 14.0
     s["logits"].scatter_(1, at, up.to(wide.dtype))
     if case["ruled"]:
