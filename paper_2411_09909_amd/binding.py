@@ -1,5 +1,5 @@
-"""Thin ctypes binding of libamxfp4.so: the same entry points as include/amxfp4.h, include/amxfp4_layer.h and
-include/amxfp4_paged.h, taking torch CUDA tensors. The calls of a serving loop, with all their buffers given, go through a small native module instead
+"""Thin ctypes binding of libamxfp4.so: the same entry points as include/amxfp4.h, include/amxfp4_layer.h,
+include/amxfp4_paged.h and include/amxfp4_scoring.h, taking torch CUDA tensors. The calls of a serving loop, with all their buffers given, go through a small native module instead
 (csrc/calls.cpp: a cast of one row 4.8 -> 3.3 us of host time); it leaves whatever it does not take to the code here.
 
 Only argument marshalling happens here (pointers, sizes, the current HIP stream); every step of the path runs in
@@ -34,6 +34,10 @@ class AmxPagedPool(ctypes.Structure):
     _fields_ = [("pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("reserved", ctypes.c_int32), ("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
                 ("v_codes", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
+
+
+class AmxScores(ctypes.Structure):
+    _fields_ = [("cap", ctypes.c_float), ("reserved", ctypes.c_int32), ("slopes", ctypes.c_void_p)]
 
 
 class AmxError(RuntimeError):
@@ -117,6 +121,17 @@ def _load():
     L.amxfp4_attention_workspace_bytes.restype = ctypes.c_size_t
     L.amxfp4_attention.argtypes = [fp, i64, i64, i64, i64, i64, vp, vp, vp, vp, vp, vp, f32, i32, vp, vp,
                                    ctypes.c_size_t, vp]
+    sp = ctypes.POINTER(AmxScores)
+    L.amxfp4_attention_masked.argtypes = [fp, i64, i64, i64, i64, i64, vp, vp, vp, vp, vp, vp, f32, sp, i32, i64, vp, vp, vp, vp,
+                                          ctypes.c_size_t, vp]
+    L.amxfp4_attention_masked.restype = ctypes.c_int
+    L.amxfp4_paged_attention_scored.argtypes = [fp, ctypes.POINTER(AmxPagedPool), vp, i64, i64, vp, i64, i64, vp, vp, vp, f32, sp, i64, vp, vp,
+                                                ctypes.c_size_t, vp]
+    L.amxfp4_paged_attention_scored.restype = ctypes.c_int
+    L.amxfp4_token_logprobs_workspace_bytes.argtypes = [i32, i64, i64, i64]
+    L.amxfp4_token_logprobs_workspace_bytes.restype = ctypes.c_size_t
+    L.amxfp4_token_logprobs.argtypes = [vp, i32, i64, i64, i64, vp, f32, i64, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    L.amxfp4_token_logprobs.restype = ctypes.c_int
     L.amxfp4_attention.restype = ctypes.c_int
     L.amxfp4_attention_merged.argtypes = L.amxfp4_attention.argtypes
     L.amxfp4_attention_merged.restype = ctypes.c_int
@@ -815,11 +830,12 @@ def paged_attention_workspace_bytes(fmt, pool, rows, q_heads, seqs, max_keys):
     return int(load().amxfp4_paged_attention_workspace_bytes(ctypes.byref(fmt), ctypes.byref(p), rows, q_heads, seqs, max_keys))
 
 
-def paged_attention(fmt, q, pool, table, lens, starts, positions, scale, max_keys=0, out=None, workspace=None):
+def paged_attention(fmt, q, pool, table, lens, starts, positions, scale, max_keys=0, out=None, workspace=None, cap=0.0, slopes=None):
     """amxfp4_paged_attention: q BF16 [rows, q_heads, head_dim] against what the rows' sequences hold in the pool (lens, starts
     and positions out of paged_plan()). max_keys: at least the longest sequence, 0 if not known. Returns BF16 [rows, q_heads *
-    head_dim]; rows behind the last sequence's are left as they were (zeros in a new tensor)."""
-    if out is not None and workspace is not None:
+    head_dim]; rows behind the last sequence's are left as they were (zeros in a new tensor). cap, slopes: amxfp4_paged_attention_scored, as for
+    attention_masked()."""
+    if out is not None and workspace is not None and not cap and slopes is None:
         rc = (_calls or _bound()).paged_attention(fmt, q, pool, table, lens, starts, positions, float(scale), max_keys, out, workspace)
         if rc is not None:
             return out if rc == 0 else _check(rc)
@@ -841,8 +857,98 @@ def paged_attention(fmt, q, pool, table, lens, starts, positions, scale, max_key
         need = int(load().amxfp4_paged_attention_workspace_bytes(ctypes.byref(fmt), ctypes.byref(p), rows, q_heads, seqs, max_keys))
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
     _here(out, workspace)
-    _check(load().amxfp4_paged_attention(ctypes.byref(fmt), ctypes.byref(p), q.data_ptr(), rows, q_heads, table.data_ptr(), seqs,
-                                         table.shape[1], lens.data_ptr(), starts.data_ptr(), positions.data_ptr(), float(scale),
-                                         int(max_keys), out.data_ptr(), workspace.data_ptr(),
-                                         workspace.numel() * workspace.element_size(), _stream()))
+    _check(load().amxfp4_paged_attention_scored(ctypes.byref(fmt), ctypes.byref(p), q.data_ptr(), rows, q_heads, table.data_ptr(), seqs,
+                                                table.shape[1], lens.data_ptr(), starts.data_ptr(), positions.data_ptr(), float(scale),
+                                                _scores(cap, slopes, q_heads), int(max_keys), out.data_ptr(), workspace.data_ptr(),
+                                                workspace.numel() * workspace.element_size(), _stream()))
+    return out
+
+
+def _scores(cap, slopes, q_heads):
+    """amx_scores_t of a call, None for scores as they are."""
+    if slopes is not None:
+        _here(slopes)
+        if slopes.dtype != torch.float32 or slopes.dim() != 1 or slopes.numel() != q_heads:
+            raise AmxError("slopes must be float32 [%d], not %s of %s" % (q_heads, slopes.dtype, tuple(slopes.shape)))
+    elif not cap:
+        return None
+    return ctypes.byref(AmxScores(float(cap), 0, None if slopes is None else slopes.data_ptr()))
+
+
+def attention_masked(fmt, q_codes, q_scales, k_codes, k_scales, v_codes, v_scales, scale, causal=True, pos0=0, first=None, last=None,
+                     cap=0.0, slopes=None, out=None, workspace=None):
+    """amxfp4_attention_masked: attention(.., merged=True) whose query row i, at position pos0 + i, sees the keys from first[i] to
+    last[i] (int32 [Sq], or None: all) and, with `causal`, none behind its position. cap > 0: scores s become cap tanh(s / cap); slopes float32
+    [q_heads]: they fall by slopes[h] for each key of distance. Operands as for attention() (contiguous). Returns BF16 [Sq, q_heads * head_dim];
+    rows that see nothing are zeros."""
+    operands = (q_codes, q_scales, k_codes, k_scales, v_codes, v_scales)
+    _here(*operands)
+    if any(t.dtype != torch.uint8 for t in operands) or any(t.dim() != 3 for t in operands[::2]):
+        raise AmxError("attention_masked: uint8 operands, codes of three dimensions")
+    q_heads, Sq, half = q_codes.shape
+    kv_heads, Sk = k_codes.shape[:2]
+    D, pair = half * 2, (2,) if fmt.asymmetric else ()
+    for name, codes, scales, shape in (("q", q_codes, q_scales, (q_heads, Sq, D)), ("k", k_codes, k_scales, (kv_heads, Sk, D)),
+                                       ("v", v_codes, v_scales, (kv_heads, D, Sk))):
+        if tuple(codes.shape) != shape[:2] + (shape[2] // 2,) or tuple(scales.shape) != shape[:2] + (shape[2] // 32,) + pair:
+            raise AmxError("attention_masked: %s codes %s and scales %s do not go with %s values in this format" % (
+                name, tuple(codes.shape), tuple(scales.shape), shape))
+    for t in (first, last):
+        if t is not None:
+            _here(t)
+            _ints(Sq, t)
+    if out is None:
+        out = torch.empty((Sq, q_heads * D), dtype=torch.bfloat16, device=q_codes.device)
+    if workspace is None:
+        workspace = torch.empty(max(256, attention_workspace_bytes(fmt, q_heads, kv_heads, Sq, Sk, D)), dtype=torch.uint8, device=q_codes.device)
+    _here(out, workspace)
+    if out.dtype != torch.bfloat16 or out.numel() != Sq * q_heads * D:
+        raise AmxError("attention_masked: out must be bfloat16 [%d, %d]" % (Sq, q_heads * D))
+    _check(load().amxfp4_attention_masked(ctypes.byref(fmt), q_heads, kv_heads, Sq, Sk, D, *(t.data_ptr() for t in operands), float(scale),
+                                          _scores(cap, slopes, q_heads), int(causal), int(pos0), None if first is None else first.data_ptr(),
+                                          None if last is None else last.data_ptr(), out.data_ptr(), workspace.data_ptr(),
+                                          workspace.numel() * workspace.element_size(), _stream()))
+    return out
+
+
+class TokenLogprobs(NamedTuple):
+    """What token_logprobs() says of each row; logprobs is None without targets, the last two without `top`."""
+    logprobs: torch.Tensor
+    entropy: torch.Tensor
+    top_logprobs: torch.Tensor
+    top_ids: torch.Tensor
+
+
+def token_logprobs_workspace_bytes(logits, top=0):
+    return int(load().amxfp4_token_logprobs_workspace_bytes(1 if logits.dtype == torch.bfloat16 else 0, *logits.shape, top))
+
+
+def token_logprobs(logits, targets=None, top=0, cap=0.0, out=None, workspace=None):
+    """amxfp4_token_logprobs: float32 or BF16 logits [rows, vocab] (rows any distance apart) -> TokenLogprobs: the log probability of each
+    row's target (int32 [rows]; 0 for one outside the vocabulary), the row's entropy, and the log probabilities and ids of its `top` largest
+    logits. cap > 0: logits x become cap tanh(x / cap) first. out: the buffers of a TokenLogprobs, float32 and int32."""
+    _need_cuda(logits)
+    if logits.dtype not in (torch.float32, torch.bfloat16) or logits.dim() != 2 or (logits.stride(1) != 1 and logits.shape[1] > 1):
+        raise AmxError("token_logprobs: float32 or bfloat16 logits [rows, vocab] with contiguous rows")
+    rows, vocab = logits.shape
+    if targets is not None:
+        _here(targets)
+        _ints(rows, targets)
+    if out is None:
+        f = lambda *shape: torch.empty(shape, dtype=torch.float32, device=logits.device)  # noqa: E731
+        out = (None if targets is None else f(rows), f(rows)) + (
+            (f(rows, top), torch.empty((rows, top), dtype=torch.int32, device=logits.device)) if top else (None, None))
+    out = TokenLogprobs(*out)
+    for t, dtype, shape in zip(out, (torch.float32,) * 3 + (torch.int32,), ((rows,), (rows,), (rows, top), (rows, top))):
+        if t is not None:
+            _here(t)
+            if t.dtype != dtype or tuple(t.shape) != shape:
+                raise AmxError("token_logprobs: an output of %s must be %s, not %s of %s" % (shape, dtype, t.dtype, tuple(t.shape)))
+    if workspace is None:
+        workspace = torch.empty(max(256, token_logprobs_workspace_bytes(logits, top)), dtype=torch.uint8, device=logits.device)
+    _here(logits[:0], workspace)
+    at = [None if t is None or t.numel() == 0 else t.data_ptr() for t in (targets,) + out]
+    _check(load().amxfp4_token_logprobs(logits.data_ptr(), 1 if logits.dtype == torch.bfloat16 else 0, rows, vocab,
+                                        logits.stride(0) if rows > 1 else vocab, at[0], float(cap), int(top), at[1], at[2], at[3], at[4],
+                                        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
     return out

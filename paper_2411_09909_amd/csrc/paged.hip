@@ -8,6 +8,7 @@
 #include "kernels.h"
 #include "layer_math.h"
 #include "paged.h"
+#include "scoring.h"
 
 namespace amx {
 namespace {
@@ -486,10 +487,10 @@ size_t amxfp4_paged_attention_workspace_bytes(const amx_format_t* fmt, const amx
   return paged_attention_workspace(pool->head_dim, rows, q_heads, pool->kv_heads, seqs, max_keys);
 }
 
-int amxfp4_paged_attention(const amx_format_t* fmt, const amx_paged_pool_t* pool, const void* q_bf16, int64_t rows, int64_t q_heads,
-                           const int32_t* table, int64_t seqs, int64_t max_pages, const int32_t* lens, const int32_t* starts,
-                           const int32_t* positions, float scale, int64_t max_keys, void* out_bf16, void* workspace,
-                           size_t workspace_bytes, void* stream) {
+int amxfp4_paged_attention_scored(const amx_format_t* fmt, const amx_paged_pool_t* pool, const void* q_bf16, int64_t rows,
+                                  int64_t q_heads, const int32_t* table, int64_t seqs, int64_t max_pages, const int32_t* lens,
+                                  const int32_t* starts, const int32_t* positions, float scale, const amx_scores_t* scores,
+                                  int64_t max_keys, void* out_bf16, void* workspace, size_t workspace_bytes, void* stream) {
   if (int rc = check(fmt, pool); rc != AMX_OK) return rc;
   if (int rc = check_memory(pool); rc != AMX_OK) return rc;
   if (!q_bf16 || !table || !lens || !starts || !positions || !out_bf16)
@@ -500,6 +501,10 @@ int amxfp4_paged_attention(const amx_format_t* fmt, const amx_paged_pool_t* pool
     return report_error(AMX_ERR_INVALID_ARG, "paged_attention: bad shape (q_heads a multiple of kv_heads, 1 to 4096 sequences)");
   // (the kernel's scale is this times log2 e, which has to be finite too)
   if (!(scale > 0.f) || scale > 0x1p127f) return report_error(AMX_ERR_INVALID_ARG, "paged_attention: scale must be positive, at most 2^127");
+  if (!scores_valid(scores))
+    return report_error(AMX_ERR_INVALID_ARG, "paged_attention: cap must be 0 or 2^-20 to 2^20, slopes 4-byte aligned, reserved 0");
+  if (scores && scores->cap > 0.f && scale > 0x1p100f)
+    return report_error(AMX_ERR_INVALID_ARG, "paged_attention: scale must be at most 2^100 where scores are capped");
   if (!aligned16(q_bf16) || !aligned16(out_bf16) || !aligned4(table) || !aligned4(lens) || !aligned4(starts) || !aligned4(positions))
     return report_error(AMX_ERR_INVALID_ARG, "paged_attention: q and out must be 16-byte aligned");
   const size_t need = paged_attention_workspace(pool->head_dim, rows, q_heads, pool->kv_heads, seqs, max_keys);
@@ -507,9 +512,17 @@ int amxfp4_paged_attention(const amx_format_t* fmt, const amx_paged_pool_t* pool
     return report_error(AMX_ERR_WORKSPACE, "paged_attention: workspace missing, too small or not 256-byte aligned");
   const hipError_t e =
       launch_paged_attention(fmt->scale, fmt->asymmetric != 0, pool->head_dim, view(pool), static_cast<const uint16_t*>(q_bf16), rows,
-                             q_heads, table, seqs, max_pages, lens, starts, positions, scale, max_keys,
+                             q_heads, table, seqs, max_pages, lens, starts, positions, scale, scores, max_keys,
                              static_cast<uint16_t*>(out_bf16), workspace, reinterpret_cast<hipStream_t>(stream));
   return e == hipSuccess ? AMX_OK : report_hip_error(e, "paged_attention launch");
+}
+
+int amxfp4_paged_attention(const amx_format_t* fmt, const amx_paged_pool_t* pool, const void* q_bf16, int64_t rows, int64_t q_heads,
+                           const int32_t* table, int64_t seqs, int64_t max_pages, const int32_t* lens, const int32_t* starts,
+                           const int32_t* positions, float scale, int64_t max_keys, void* out_bf16, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  return amxfp4_paged_attention_scored(fmt, pool, q_bf16, rows, q_heads, table, seqs, max_pages, lens, starts, positions, scale, nullptr,
+                                       max_keys, out_bf16, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

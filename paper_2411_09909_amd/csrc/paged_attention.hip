@@ -35,6 +35,7 @@
 
 #include "kernels.h"
 #include "layer_math.h"
+#include "scoring.h"
 
 namespace amx {
 namespace {
@@ -67,6 +68,7 @@ struct PagedWork {
   int seqs, q_heads, per;  // per: query heads to a key head
   float scale_log2;
   int whole, unit_log2;    // tiles of 64 tokens to a unit
+  Scores scores;           // of a launch that caps scores or lets them fall with distance
 };
 
 // What a workgroup leaves behind for the joining kernel, at the front of the workspace.
@@ -194,8 +196,9 @@ struct PagedTile {
   u32x4 ks[GS][kScaleWords / 4], vs[GS][kScaleWords / 4];
 };
 
-// SHARE: waves to a sequence and key head, 4 or 1.
-template <int SCALE_KIND, bool ASYM, int D, int GC, int SHARE>
+// SHARE: waves to a sequence and key head, 4 or 1. SCORED: scores are capped, or fall with distance, or both (include/amxfp4_scoring.h); they
+// are in units of log2 from there on.
+template <int SCALE_KIND, bool ASYM, int D, int GC, int SHARE, bool SCORED>
 __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 : 2) void paged_attention_kernel(
     PagedPool pool, PagedWork w, const int32_t* __restrict__ table, const int32_t* __restrict__ lens, const int32_t* __restrict__ starts,
     const int32_t* __restrict__ positions) {
@@ -400,7 +403,9 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i] = f32x4{0, 0, 0, 0};
     float m = -INFINITY, l = 0.f;
-    const float sc = w.scale_log2;
+    const float sc = SCORED ? 1.0f : w.scale_log2;
+    float slope = 0.f;
+    if (SCORED && w.scores.slopes) slope = asked ? w.scores.slopes[(uint32_t)head * (uint32_t)w.per + head_of] * kLog2e : 0.f;
 
     for (; tile < stop; tile += SHARE) {
       const bool more = tile + SHARE < stop;
@@ -487,6 +492,20 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
       } else {
 #pragma unroll
         for (int k = 0; k < 16; ++k) y[k] = x[k];
+      }
+      if constexpr (SCORED) {
+        if (w.scores.cap > 0.f) {
+#pragma unroll
+          for (int k = 0; k < kMine; ++k) y[k] = capped(y[k], w.scores.in, w.scores.cap);
+        } else {
+#pragma unroll
+          for (int k = 0; k < kMine; ++k) y[k] *= w.scores.scale;
+        }
+        if (w.scores.slopes) {  // (keys from the row's last one on are not seen: no distance below 0 counts)
+          const float away = (float)(limit - 1 - first - 16 * u - gc);
+#pragma unroll
+          for (int k = 0; k < kMine; ++k) y[k] = __builtin_fmaf(-slope, away - (float)(GC * k), y[k]);
+        }
       }
       if (!all) {
 #pragma unroll
@@ -760,8 +779,8 @@ size_t paged_attention_workspace(int head_dim, int64_t rows, int64_t q_heads, in
 
 hipError_t launch_paged_attention(int scale_kind, bool asym, int head_dim, const PagedPool& pool, const uint16_t* q, int64_t rows,
                                   int64_t q_heads, const int32_t* table, int64_t seqs, int64_t max_pages, const int32_t* lens,
-                                  const int32_t* starts, const int32_t* positions, float scale, int64_t max_keys, uint16_t* out,
-                                  void* workspace, hipStream_t s) {
+                                  const int32_t* starts, const int32_t* positions, float scale, const amx_scores_t* scores,
+                                  int64_t max_keys, uint16_t* out, void* workspace, hipStream_t s) {
   const int64_t per = q_heads / pool.kv_heads, width = max_pages << pool.page_log2;
   const int64_t most_keys = max_keys > 0 && max_keys < width ? max_keys : width;
   const int gc = columns_of(head_dim, rows, seqs, per), nc = 16 / gc;
@@ -771,7 +790,8 @@ hipError_t launch_paged_attention(int scale_kind, bool asym, int head_dim, const
   int unit_log2 = 0;
   while (tiles >= (int64_t(1) << 31) / ((tokens >> unit_log2) + 1 + kStart)) ++unit_log2;
   const PagedWork w = {q, out, static_cast<uint8_t*>(workspace), rows, max_pages, (int)seqs, (int)q_heads, (int)per,
-                       scale * 1.4426950408889634f, whole ? 1 : 0, unit_log2};
+                       scale * kLog2e, whole ? 1 : 0, unit_log2, scores_of(scores, scale)};
+  const bool scored = w.scores.cap > 0.f || w.scores.slopes;
   const size_t values = 4 * kTile * (size_t)head_dim / 2, shares = 4 * (size_t)nc * head_dim * sizeof(float);
   const int64_t segments = seqs * pool.kv_heads;
   const bool by_wave = is_by_wave(segments, most_keys);
@@ -788,11 +808,14 @@ hipError_t launch_paged_attention(int scale_kind, bool asym, int head_dim, const
     grid = dim3((unsigned)workers);
     lds += sequences_bytes(seqs);
   }
-  auto go = [&]<int SK, bool ASYM, int D, int GC>() {
+  auto attend = [&]<int SK, bool ASYM, int D, int GC, bool SCORED>() {
     if (!by_wave)
-      hipLaunchKernelGGL((paged_attention_kernel<SK, ASYM, D, GC, 4>), grid, dim3(256), lds, s, pool, w, table, lens, starts, positions);
+      hipLaunchKernelGGL((paged_attention_kernel<SK, ASYM, D, GC, 4, SCORED>), grid, dim3(256), lds, s, pool, w, table, lens, starts, positions);
     else
-      hipLaunchKernelGGL((paged_attention_kernel<SK, ASYM, D, GC, 1>), grid, dim3(256), lds, s, pool, w, table, lens, starts, positions);
+      hipLaunchKernelGGL((paged_attention_kernel<SK, ASYM, D, GC, 1, SCORED>), grid, dim3(256), lds, s, pool, w, table, lens, starts, positions);
+  };
+  auto go = [&]<int SK, bool ASYM, int D, int GC>() {
+    scored ? attend.template operator()<SK, ASYM, D, GC, true>() : attend.template operator()<SK, ASYM, D, GC, false>();
     if (whole) return hipGetLastError();
     constexpr int kSlices = join_slices(16 / GC * D);
     if (kSlices > 1 && tiles <= kSlicedTiles)

@@ -1,0 +1,419 @@
+// Log probabilities of given tokens, entropy and the likeliest alternatives out of logits (include/amxfp4_scoring.h), in one
+// pass over them.
+//
+// With y the logit (or the capped one), a thread keeps of what it has read the maximum m and, against it,
+//     S = sum e^(y - m)   and   T = sum e^(y - m) (y - m);
+// two such triples join at M = max(m, m'):  S + S' with factors f = e^(m - M), and T as f (T + S (m - M)) + .... At the end
+//     logprob = (y_t - m) - log S,   entropy = log S - T / S.
+// (Differences first and log2 e after them: the largest logit's is exactly 0, whatever its size.)
+//
+// Alternatives. A row is read in segments (4 chunks of 16 bytes to a lane, side by side over the wave); each leaves its largest logit
+// in LDS, each thread its own. The `top` best elements lie in the `top` best segments (by their largest, the earlier of equal
+// ones: every better segment holds an element that is better than all of a worse one's), and are not below the top-th largest of
+// the segments' or of the threads' maxima. So only those segments are read again, from the cache, and the few elements at or above that
+// bound are put in order by counting for each how many are better. Rows in which more than kList elements reach the bound
+// (equal logits by the hundred, fewer tokens than `top` not ruled out) take them one after the other.
+#include "kernels.h"
+#include "scoring.h"
+
+namespace amx {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kChunks = 4;      // of 16 bytes, to a lane and segment
+constexpr int kSegments = 512;  // of a part, at most
+constexpr int kList = 512;      // candidates that are put in order at once
+constexpr int kMostTop = 64;
+constexpr int kMostParts = 64;
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct Sums {
+  float m, s, t;
+};
+__device__ __forceinline__ Sums joined(Sums a, Sums b) {
+  const float m = fmaxf(a.m, b.m), to = m == -INFINITY ? 0.f : m;
+  // (nothing in one: sums of 0, or NaN; far below the other: 0 times a number)
+  const float da = a.m == -INFINITY ? 0.f : fmaxf(a.m - to, -1000.f), db = b.m == -INFINITY ? 0.f : fmaxf(b.m - to, -1000.f);
+  const float fa = __builtin_amdgcn_exp2f(da * kLog2e), fb = __builtin_amdgcn_exp2f(db * kLog2e);
+  return {m, a.s * fa + b.s * fb, (a.t + a.s * da) * fa + (b.t + b.s * db) * fb};
+}
+
+__device__ __forceinline__ bool is_better(float v, int i, float w, int j) { return v > w || (v == w && i < j); }
+
+struct LogprobWork {
+  const void* logits;
+  const int32_t* targets;
+  float *logprob, *entropy, *top_logprobs;
+  int32_t* top_ids;
+  int64_t ld;
+  int vocab, top, parts, per_part;  // per_part: segments
+  float in, cap;                    // as in Scores, the cap itself
+  float4* sums;                     // workspace: (m, S, T) of each row and part
+  uint2* tops;                      // workspace: (logit, id) [row][part][top], best first
+};
+
+// A logit, capped; -inf stays.
+template <bool CAP>
+__device__ __forceinline__ float value_of(const LogprobWork& w, float x) {
+  if constexpr (CAP) return x == -INFINITY ? x : capped(x, w.in, w.cap);
+  return x;
+}
+
+struct Selection {
+  float best[kThreads];
+  float list_v[kList];
+  int list_i[kList];
+  float wave_v[kWaves];
+  int wave_i[kWaves];
+  int count;
+  float bound;
+};
+
+// The k best of the elements that each(f) hands to this thread as f(logit, id), k in all threads together, in order: emit(rank, logit, id).
+// No element below `bound` is among them. What is not there (of rows with NaN) comes out as id -1.
+template <class Each, class Emit>
+__device__ __forceinline__ void select_best(Selection& l, int k, float bound, Each each, Emit emit) {
+  const int t = threadIdx.x;
+  if (t == 0) l.count = 0;
+  __syncthreads();
+  each([&](float v, int i) {
+    if (v >= bound) {
+      const int at = atomicAdd(&l.count, 1);
+      if (at < kList) l.list_v[at] = v, l.list_i[at] = i;
+    }
+  });
+  __syncthreads();
+  const int n = l.count;
+  if (n <= kList) {
+    for (int c = t; c < n; c += kThreads) {
+      const float v = l.list_v[c];
+      const int i = l.list_i[c];
+      int rank = 0;
+      for (int o = 0; o < n; ++o) rank += is_better(l.list_v[o], l.list_i[o], v, i) ? 1 : 0;
+      if (rank < k) emit(rank, v, i);
+    }
+    for (int r = n + t; r < k; r += kThreads) emit(r, NAN, -1);
+    return;
+  }
+  float last_v = INFINITY;
+  int last_i = -1;
+  for (int r = 0; r < k; ++r) {
+    float v = -INFINITY;
+    int i = 0x7FFFFFFF;
+    each([&](float x, int j) {
+      if (is_better(last_v, last_i, x, j) && is_better(x, j, v, i)) v = x, i = j;
+    });
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const float ov = __shfl_xor(v, o, 64);
+      const int oi = __shfl_xor(i, o, 64);
+      if (is_better(ov, oi, v, i)) v = ov, i = oi;
+    }
+    __syncthreads();  // (the last round's have been read)
+    if ((t & 63) == 0) l.wave_v[t >> 6] = v, l.wave_i[t >> 6] = i;
+    __syncthreads();
+#pragma unroll
+    for (int o = 0; o < kWaves; ++o)
+      if (is_better(l.wave_v[o], l.wave_i[o], v, i)) v = l.wave_v[o], i = l.wave_i[o];
+    if (t == 0) emit(r, i == 0x7FFFFFFF ? NAN : v, i == 0x7FFFFFFF ? -1 : i);
+    last_v = v, last_i = i;
+  }
+}
+
+// the k-th largest of n <= kThreads values (k <= n), one to a thread
+__device__ __forceinline__ float kth_largest(Selection& l, int n, int k, float mine) {
+  const int t = threadIdx.x;
+  l.best[t] = mine;
+  __syncthreads();
+  if (t < n) {
+    int rank = 0;
+    for (int o = 0; o < n; ++o) rank += is_better(l.best[o], o, mine, t) ? 1 : 0;
+    if (rank == k - 1) l.bound = mine;
+  }
+  __syncthreads();
+  return l.bound;
+}
+
+// What is left to do for a row of which everything is known: thread 0.
+template <bool CAP>
+__device__ __forceinline__ void finish(const LogprobWork& w, int64_t row, Sums all, float log_s, float target) {
+  const bool nothing = all.m == -INFINITY && all.s == 0.f;
+  if (w.targets) {
+    const int at = w.targets[row];
+    w.logprob[row] = at < 0 || at >= w.vocab ? 0.f : nothing ? -INFINITY : (value_of<CAP>(w, target) - all.m) - log_s;
+  }
+  if (w.entropy) w.entropy[row] = nothing ? 0.f : log_s - all.t / all.s;
+}
+template <bool CAP>
+__device__ __forceinline__ float logprob_of(const LogprobWork& w, Sums all, float log_s, float x) {
+  return all.m == -INFINITY && all.s == 0.f ? -INFINITY : (value_of<CAP>(w, x) - all.m) - log_s;
+}
+
+template <bool BF16, bool CAP, bool TOP>
+__global__ __launch_bounds__(kThreads) void token_logprobs_kernel(LogprobWork w) {
+  using Element = std::conditional_t<BF16, uint16_t, float>;
+  constexpr int kE = 16 / (int)sizeof(Element), kN = kChunks * kE;  // elements of a chunk; of a lane and segment
+  constexpr int kSegment = 64 * kN;
+  __shared__ Selection l;
+  __shared__ Sums wave_sums[kWaves];
+  __shared__ float segment_best[TOP ? kSegments : 1];
+  __shared__ int chosen[TOP ? kMostTop : 1];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int64_t row = blockIdx.x / (uint32_t)w.parts;
+  const int part = (int)(blockIdx.x - (uint32_t)row * (uint32_t)w.parts);
+  const Element* x = static_cast<const Element*>(w.logits) + row * w.ld;
+  // elements that lie between the 16-byte boundary before the row and its first
+  const int off = (int)((reinterpret_cast<uintptr_t>(x) & 15) / sizeof(Element));
+  const int s0 = part * w.per_part, s1 = min(s0 + w.per_part, (w.vocab + off + kSegment - 1) / kSegment);
+  auto value = [&](Element e) { if constexpr (BF16) return u2f((uint32_t)e << 16); else return e; };
+  float target = 0.f;  // (asked for now: it is here when it is wanted)
+  if (t == 0 && w.parts == 1 && w.targets) {
+    const int at = w.targets[row];
+    if (at >= 0 && at < w.vocab) target = value(x[at]);
+  }
+
+  // a lane's elements of segment `s`: v[c kE + e] is element first + 64 kE c + e; outside the row -inf
+  auto load = [&](int s, float (&v)[kN]) {
+    const int first = s * kSegment - off + lane * kE;
+    if (s * kSegment - off >= 0 && (s + 1) * kSegment - off <= w.vocab) {  // uniform
+      u32x4 r[kChunks];
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) r[c] = *reinterpret_cast<const u32x4*>(x + first + c * 64 * kE);
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t word = r[c][i];
+          if constexpr (BF16)
+            v[c * kE + 2 * i] = u2f(word << 16), v[c * kE + 2 * i + 1] = u2f(word & 0xFFFF0000u);
+          else
+            v[c * kE + i] = u2f(word);
+        }
+    } else {
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+          const int i = first + c * 64 * kE + e;
+          v[c * kE + e] = i >= 0 && i < w.vocab ? value(x[i]) : -INFINITY;
+        }
+    }
+  };
+
+  // ---- the pass
+  Sums mine = {-INFINITY, 0.f, 0.f};
+  float best = -INFINITY;  // of the thread, as logits
+  for (int s = s0 + wave; s < s1; s += kWaves) {
+    float v[kN];
+    load(s, v);
+    float most = v[0];
+#pragma unroll
+    for (int i = 1; i < kN; ++i) most = fmaxf(most, v[i]);
+    most = fmaxf(most, -INFINITY);  // (a NaN alone)
+    if constexpr (TOP) {
+      best = fmaxf(best, most);
+      float all = most;
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor(all, o, 64));
+      if (lane == 0) segment_best[s - s0] = all;
+    }
+    const float m = fmaxf(mine.m, value_of<CAP>(w, most)), to = m == -INFINITY ? 0.f : m;
+    const float d = mine.m == -INFINITY ? 0.f : fmaxf(mine.m - to, -1000.f), f = __builtin_amdgcn_exp2f(d * kLog2e);
+    mine.t = (mine.t + mine.s * d) * f, mine.s *= f, mine.m = m;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const float z = value_of<CAP>(w, v[i]) - to, e = __builtin_amdgcn_exp2f(z * kLog2e);
+      mine.s += e;
+      mine.t = __builtin_fmaf(e, fmaxf(z, -1000.f), mine.t);  // (0 times -inf)
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1)
+    mine = joined(mine, Sums{__shfl_xor(mine.m, o, 64), __shfl_xor(mine.s, o, 64), __shfl_xor(mine.t, o, 64)});
+  if (lane == 0) wave_sums[wave] = mine;
+  __syncthreads();
+  const Sums all = joined(joined(wave_sums[0], wave_sums[1]), joined(wave_sums[2], wave_sums[3]));
+  const float log_s = kLn2 * __builtin_amdgcn_logf(all.s);
+  if (t == 0) {
+    if (w.parts == 1)
+      finish<CAP>(w, row, all, log_s, target);
+    else
+      w.sums[blockIdx.x] = make_float4(all.m, all.s, all.t, 0.f);
+  }
+  if constexpr (TOP) {
+    const int segments = max(s1 - s0, 0), k = w.top;
+    if (t < kMostTop) chosen[t] = -1;
+    float bound = kth_largest(l, kThreads, k, best);
+    for (int s = t; s < segments; s += kThreads) {
+      const float v = segment_best[s];
+      int rank = 0;
+      for (int o = 0; o < segments; ++o) rank += is_better(segment_best[o], o, v, s) ? 1 : 0;
+      if (rank < k) chosen[rank] = s;
+    }
+    __syncthreads();
+    if (segments >= k) bound = fmaxf(bound, segment_best[chosen[k - 1]]);
+    const int count = min(segments, k);
+    auto each = [&](auto f) {
+      for (int c = wave; c < count; c += kWaves) {
+        const int s = s0 + chosen[c];
+        float v[kN];
+        load(s, v);
+        const int first = s * kSegment - off + lane * kE;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+          const int id = first + i / kE * 64 * kE + i % kE;
+          if (id >= 0 && id < w.vocab) f(v[i], id);
+        }
+      }
+    };
+    auto emit = [&](int rank, float v, int id) {
+      if (w.parts == 1)
+        w.top_logprobs[row * k + rank] = logprob_of<CAP>(w, all, log_s, v), w.top_ids[row * k + rank] = id;
+      else
+        w.tops[(int64_t)blockIdx.x * k + rank] = make_uint2(f2u(v), (uint32_t)id);
+    };
+    select_best(l, k, bound, each, emit);
+  }
+}
+
+// Adds up the parts of a row. (A part with fewer elements than `top` has ids of -1 at its end.)
+template <bool BF16, bool CAP, bool TOP>
+__global__ __launch_bounds__(kThreads) void token_logprobs_join_kernel(LogprobWork w) {
+  __shared__ Selection l;
+  __shared__ Sums total;
+  const int t = threadIdx.x, k = w.top, parts = w.parts;
+  const int64_t row = blockIdx.x;
+  if (t < 64) {
+    Sums mine = {-INFINITY, 0.f, 0.f};
+    if (t < parts) {
+      const float4 v = w.sums[row * parts + t];
+      mine = {v.x, v.y, v.z};
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1)
+      mine = joined(mine, Sums{__shfl_xor(mine.m, o, 64), __shfl_xor(mine.s, o, 64), __shfl_xor(mine.t, o, 64)});
+    if (t == 0) {
+      float target = 0.f;
+      if (w.targets) {
+        const int at = w.targets[row];
+        if (at >= 0 && at < w.vocab) {
+          if constexpr (BF16)
+            target = u2f((uint32_t)static_cast<const uint16_t*>(w.logits)[row * w.ld + at] << 16);
+          else
+            target = static_cast<const float*>(w.logits)[row * w.ld + at];
+        }
+      }
+      finish<CAP>(w, row, mine, kLn2 * __builtin_amdgcn_logf(mine.s), target);
+      total = mine;
+    }
+  }
+  if constexpr (TOP) {
+    // the parts' first `deep` elements are `top` or more: the top-th largest of them bounds the result
+    const uint2* tops = w.tops + row * parts * k;
+    const int deep = (k + parts - 1) / parts, n = deep * parts;
+    float head = -INFINITY;
+    if (t < n) {
+      const float v = u2f(tops[t / deep * k + t % deep].x);
+      head = v == v ? v : -INFINITY;
+    }
+    const float bound = kth_largest(l, n, k, head);
+    const Sums all = total;
+    const float log_s = kLn2 * __builtin_amdgcn_logf(all.s);
+    auto each = [&](auto f) {
+      for (int i = t; i < parts * k; i += kThreads) {
+        const uint2 v = tops[i];
+        if ((int)v.y >= 0) f(u2f(v.x), (int)v.y);
+      }
+    };
+    auto emit = [&](int rank, float v, int id) {
+      w.top_logprobs[row * k + rank] = logprob_of<CAP>(w, all, log_s, v), w.top_ids[row * k + rank] = id;
+    };
+    select_best(l, k, bound, each, emit);
+  }
+}
+
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+int segment_of(int dtype) { return 64 * kChunks * 16 / (dtype == 1 ? 2 : 4); }
+
+// Parts that a row is read in, and segments of each. Rows enough to fill the chip are read whole.
+int parts_of(int dtype, int64_t rows, int64_t vocab, int& per_part) {
+  const int64_t segments = (vocab + 7 + segment_of(dtype) - 1) / segment_of(dtype);  // (a row may begin up to 7 elements behind a boundary)
+  int64_t parts = (2048 + rows - 1) / rows;
+  const int64_t most = (segments + kWaves - 1) / kWaves, least = (segments + kSegments - 1) / kSegments;
+  parts = parts < most ? parts : most;
+  parts = parts < kMostParts ? parts : kMostParts;
+  parts = parts > least ? parts : least;
+  per_part = (int)((segments + parts - 1) / parts);
+  return (int)((segments + per_part - 1) / per_part);
+}
+
+constexpr int64_t kMostVocab = int64_t(1) << 24, kMostRows = int64_t(1) << 23;
+static_assert(kMostVocab / 1024 / kSegments < kMostParts, "a part's segments fit");
+
+bool bad_shape(int32_t dtype, int64_t rows, int64_t vocab, int64_t top) {
+  return (dtype != 0 && dtype != 1) || rows <= 0 || rows > kMostRows || vocab <= 0 || vocab > kMostVocab || top < 0 || top > kMostTop || top > vocab;
+}
+
+size_t sums_bytes(int64_t rows, int parts) { return ((size_t)rows * parts * sizeof(float4) + 255) & ~(size_t)255; }
+
+}  // namespace
+}  // namespace amx
+
+using namespace amx;
+
+extern "C" {
+
+size_t amxfp4_token_logprobs_workspace_bytes(int32_t dtype, int64_t rows, int64_t vocab, int64_t top) {
+  if (bad_shape(dtype, rows, vocab, top)) return 0;
+  int per_part;
+  const int parts = parts_of(dtype, rows, vocab, per_part);
+  return parts == 1 ? 0 : sums_bytes(rows, parts) + (size_t)rows * parts * top * sizeof(uint2);
+}
+
+int amxfp4_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, const int32_t* targets, float cap,
+                          int64_t top, float* logprob, float* entropy, float* top_logprobs, int32_t* top_ids, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  if (!logits) return report_error(AMX_ERR_INVALID_ARG, "token_logprobs: logits is NULL");
+  if (bad_shape(dtype, rows, vocab, top))
+    return report_error(AMX_ERR_INVALID_ARG, "token_logprobs: dtype 0 or 1, 1 to 2^23 rows and 2^24 columns, top 0 to 64 and at most vocab");
+  if (ld < vocab || ld > (int64_t(1) << 31) || rows > (int64_t(1) << 40) / ld)
+    return report_error(AMX_ERR_INVALID_ARG, "token_logprobs: ld at least vocab, at most 2^31, rows * ld at most 2^40");
+  if (!(targets == nullptr) != !(logprob == nullptr))
+    return report_error(AMX_ERR_INVALID_ARG, "token_logprobs: targets and logprob go together");
+  if ((top > 0) != (top_logprobs != nullptr) || (top > 0) != (top_ids != nullptr))
+    return report_error(AMX_ERR_INVALID_ARG, "token_logprobs: top_logprobs and top_ids are wanted exactly when top is positive");
+  if (!targets && !entropy && !top) return report_error(AMX_ERR_INVALID_ARG, "token_logprobs: nothing is asked for");
+  if (!(cap == 0.f || (cap >= 0x1p-20f && cap <= 0x1p20f)))
+    return report_error(AMX_ERR_INVALID_ARG, "token_logprobs: cap must be 0 or 2^-20 to 2^20");
+  if (!aligned(logits, dtype == 1 ? 2 : 4) || !aligned(targets, 4) || !aligned(logprob, 4) || !aligned(entropy, 4) ||
+      !aligned(top_logprobs, 4) || !aligned(top_ids, 4))
+    return report_error(AMX_ERR_INVALID_ARG, "token_logprobs: pointers must be aligned to their elements");
+  LogprobWork w = {logits, targets, logprob, entropy, top_logprobs, top_ids, ld, (int)vocab, (int)top, 0, 0, 0.f, 0.f, nullptr, nullptr};
+  w.parts = parts_of(dtype, rows, vocab, w.per_part);
+  if (cap > 0.f) w.in = 2 * kLog2e / cap, w.cap = cap;
+  if (w.parts > 1) {
+    if (!workspace || workspace_bytes < amxfp4_token_logprobs_workspace_bytes(dtype, rows, vocab, top) || !aligned(workspace, 256))
+      return report_error(AMX_ERR_WORKSPACE, "token_logprobs: workspace missing, too small or not 256-byte aligned");
+    w.sums = static_cast<float4*>(workspace);
+    w.tops = reinterpret_cast<uint2*>(static_cast<uint8_t*>(workspace) + sums_bytes(rows, w.parts));
+  }
+  auto go = [&]<bool BF16, bool CAP, bool TOP>() {
+    const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    hipLaunchKernelGGL((token_logprobs_kernel<BF16, CAP, TOP>), dim3((unsigned)(rows * w.parts)), dim3(kThreads), 0, s, w);
+    if (w.parts > 1) hipLaunchKernelGGL((token_logprobs_join_kernel<BF16, CAP, TOP>), dim3((unsigned)rows), dim3(kThreads), 0, s, w);
+  };
+  auto with_type = [&]<bool BF16>() {
+    if (cap > 0.f)
+      top ? go.template operator()<BF16, true, true>() : go.template operator()<BF16, true, false>();
+    else
+      top ? go.template operator()<BF16, false, true>() : go.template operator()<BF16, false, false>();
+  };
+  dtype == 1 ? with_type.template operator()<true>() : with_type.template operator()<false>();
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? AMX_OK : report_hip_error(e, "token_logprobs launch");
+}
+
+}  // extern "C"

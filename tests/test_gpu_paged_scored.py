@@ -1,0 +1,111 @@
+"""Attention over the paged cache with capped scores and biases that fall with distance, against 64 bits over the cache's bytes; what may be
+off as in test_gpu_paged.allowed(), the size of a score counting the cap and the distances' share too."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import scoring_ref
+from paper_2411_09909_amd import binding
+from tests.test_gpu_attention_masked import slopes_of
+from tests.test_gpu_paged import FORMATS, allowed, bits, dev, f64, filled, host_pool
+
+pytestmark = pytest.mark.gpu
+
+
+def check(seed, name, H, G, D, page, lens, rows, cap, slopes, max_keys=0, spare=0, positions=None, gain=1.0):
+    rng = np.random.RandomState(seed)
+    kind, asym = FORMATS[name]
+    fmt, pool, table = filled(rng, name, G, D, page, lens, max(1, -(-max(lens) // page)))
+    starts = np.concatenate([[0], np.cumsum(rows)])
+    T = int(starts[-1]) + spare
+    if positions is None:
+        positions = np.concatenate([np.arange(n - r, n) for n, r in zip(lens, rows)] + [np.full(spare, -1)])
+    q = torch.from_numpy((rng.randn(T, H, D) * gain).astype(np.float32)).to(torch.bfloat16).cuda()
+    out = torch.full((T, H * D), 7.0, dtype=torch.bfloat16, device="cuda")
+    need = binding.paged_attention_workspace_bytes(fmt, pool, T, H, len(lens), max_keys)
+    ws = torch.full((need + 4096,), 0xFF, dtype=torch.uint8, device="cuda")
+    args = (fmt, q, pool, dev(table), dev(lens), dev(starts), dev(positions), 1 / math.sqrt(D))
+    how = dict(max_keys=max_keys, cap=cap, slopes=None if slopes is None else torch.from_numpy(slopes).cuda())
+    binding.paged_attention(*args, **how, out=out, workspace=ws[:need])
+    assert (ws[need:] == 0xFF).all()
+    got = f64(bits(out)).reshape(T, H, D)
+    want, weight, size = scoring_ref.paged_attention(f64(bits(q)).reshape(T, H, D), host_pool(pool), table, lens, starts, positions, 1 / math.sqrt(D),
+                                                     kind, asym, cap, slopes)
+    none = np.isnan(want)
+    assert (got[none] == 7.0).all()
+    over = np.where(none, 0, np.abs(got - want) / allowed(want, weight, size[..., None], D))
+    print("%.3f of what is allowed" % over.max())
+    assert over.max() <= 1
+    again = binding.paged_attention(*args, **how, workspace=torch.zeros(need + 256, dtype=torch.uint8, device="cuda"))
+    assert torch.equal(again[:starts[-1]], out[:starts[-1]])
+
+
+SCORES = [(20.0, False), (0.0, True), (3.0, True)]
+
+
+@pytest.mark.parametrize("name", FORMATS)
+@pytest.mark.parametrize("H,G,D", [(8, 2, 128), (12, 12, 64), (16, 2, 128), (16, 1, 64)])
+@pytest.mark.parametrize("cap,sloped", SCORES)
+def test_formats_and_heads(name, H, G, D, cap, sloped):
+    check(len(name) + D, name, H, G, D, 32, [1, 33, 200, 64, 129], [1] * 5, cap, slopes_of(H) if sloped else None)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("cap,sloped", SCORES)
+def test_lengths_rows_and_spare_rows(D, cap, sloped):
+    lens = [0, 1, 2, 15, 16, 17, 63, 64, 65, 128, 257, 700]
+    check(D, "amxfp4_e5m2", 8, 2, D, 16, lens, [0] + [1] * 11, cap, slopes_of(8) if sloped else None, spare=2)
+    check(D, "amxfp4_e5m2", 6, 2, D, 64, [90, 3, 40], [4, 0, 31], cap, slopes_of(6) if sloped else None, spare=1)
+
+
+@pytest.mark.parametrize("name,H,G,D", [("amxfp4_e5m2", 8, 2, 128), ("mxfp4_e8m0", 4, 4, 64), ("amxfp4_e4m3", 32, 2, 128)])
+@pytest.mark.parametrize("cap,sloped", SCORES)
+def test_split_over_workgroups_and_by_the_wave(name, H, G, D, cap, sloped):
+    s = slopes_of(H) if sloped else None
+    check(1, name, H, G, D, 64, [5000], [1], cap, s, max_keys=5000)
+    check(2, name, H, G, D, 64, [3000, 2999, 4097, 6], [1, 2, 1, 3], cap, s)
+    check(3, name, G, G, D, 16, [40, 7, 64, 90] * 30, [1] * 120, cap, slopes_of(G) if sloped else None, max_keys=90)
+
+
+@pytest.mark.parametrize("cap,sloped", SCORES)
+def test_positions_that_are_none_or_beyond_the_tokens(cap, sloped):
+    """A position behind the sequence's end counts as its last token's: all distances shift alike."""
+    s = slopes_of(8) if sloped else None
+    check(4, "amxfp4_e5m2", 8, 2, 128, 32, [100, 50, 30], [2, 2, 1], cap, s, positions=[98, 2 ** 31 - 1, -1, 200, -2 ** 31])
+
+
+def test_large_scores_and_steep_slopes():
+    check(5, "amxfp4_e5m2", 4, 1, 128, 32, [300, 77], [1, 1], 50.0, None, gain=60.0)
+    check(6, "amxfp4_e8m0", 4, 1, 64, 32, [300, 77], [1, 1], 0.0, np.array([20.0, -0.3, 0.0, 1.0], np.float32))
+
+
+def test_slopes_of_zero_and_a_wide_cap_change_little():
+    rng = np.random.RandomState(9)
+    fmt, pool, table = filled(rng, "amxfp4_e5m2", 2, 128, 32, [500, 60], 16)
+    q = torch.randn(2, 8, 128, device="cuda").to(torch.bfloat16)
+    args = (fmt, q, pool, dev(table), dev([500, 60]), dev([0, 1, 2]), dev([499, 59]), 0.1)
+    a = binding.paged_attention(*args).float()
+    for how in (dict(slopes=torch.zeros(8, device="cuda")), dict(cap=2.0 ** 12)):
+        b = binding.paged_attention(*args, **how).float()
+        assert (a - b).norm() <= 2.0 ** -7 * a.norm()
+
+
+def test_a_graph():
+    rng = np.random.RandomState(10)
+    fmt, pool, table = filled(rng, "amxfp4_e5m2", 2, 128, 64, [3000, 1200], 48)
+    q = torch.randn(2, 8, 128, device="cuda").to(torch.bfloat16)
+    slopes = torch.from_numpy(slopes_of(8)).cuda()
+    args = (fmt, q, pool, dev(table), dev([3000, 1200]), dev([0, 1, 2]), dev([2999, 1199]), 0.1)
+    out = torch.zeros(2, 1024, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(binding.paged_attention_workspace_bytes(fmt, pool, 2, 8, 2, 0), dtype=torch.uint8, device="cuda")
+    binding.paged_attention(*args, cap=30.0, slopes=slopes)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        binding.paged_attention(*args, cap=30.0, slopes=slopes, out=out, workspace=ws)
+    for _ in range(3):
+        q.normal_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, binding.paged_attention(*args, cap=30.0, slopes=slopes))
