@@ -46,7 +46,7 @@ __device__ __forceinline__ int wave_max(int v) {
 }
 
 template <int SCALE_KIND, int D, bool CAP, bool SLOPE>
-__global__ __launch_bounds__(64 * kWaves) void attention_masked_kernel(const uint8_t* __restrict__ Q_codes, const uint8_t* __restrict__ Q_scales,
+__global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : 3) void attention_masked_kernel(const uint8_t* __restrict__ Q_codes, const uint8_t* __restrict__ Q_scales,
                                                                      int asym, const uint16_t* __restrict__ Kp,
                                                                      const uint16_t* __restrict__ Vp, uint16_t* __restrict__ out, MaskedWork w) {
   // FP8-E5M2 scales: probabilities as FP16 times 2^8, V^T biased by 2^-3, the 2^5 taken out with the row sum at the end
@@ -133,12 +133,40 @@ __global__ __launch_bounds__(64 * kWaves) void attention_masked_kernel(const uin
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
     for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
-  float m = -__builtin_inff(), l = 0.f;       // running maximum (in units of log2) and sum of this lane's query
+  // Running maximum (in units of log2) and sum of this lane's query; the sum of the keys that this lane has, until the end. The maximum
+  // starts finite: a query that has seen no key yet then has weights of 0 and a factor of 1 without any test.
+  float m = -0x1.fffffep127f, l = 0.f;
   const int row_in_tile = 4 * (lane >> 5);    // key of register v: 8 (v / 4) + row_in_tile + v % 4
-  // distances are taken from the nearest key that the query sees: all its scores shift alike, and stay small where it sees far keys only
+  // Distances are taken from the nearest key that the query sees: all its scores shift alike, and stay small where it sees far keys
+  // only. In a tile in front of all the wave's nearest keys a score is f(q.k) + slope (key in the tile) - slope (distance of the tile's first
+  // key): the second term is the last addition of f, the third is left to the maximum.
   const float slope = SLOPE ? w.scores.slopes[h] * kLog2e : 0.f;
   const int nearest = none ? 0 : max(lo, min(position, lo + (int)span));
+  const int all_nearest = SLOPE ? wave_min(none ? 0x7FFFFFFF : nearest) : 0;
+  float step[16];
+  if constexpr (SLOPE) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      // (in scalar registers: an instruction takes one of those, and the scale is the one to move)
+      float of = slope * (float)(8 * (v >> 2) + (v & 3));
+      asm volatile("" : "+v"(of));
+      step[v] = u2f((uint32_t)__builtin_amdgcn_readfirstlane((int)f2u(of)));
+    }
+  }
+  float scale = w.scores.scale;
+  if constexpr (SLOPE && !CAP) asm volatile("" : "+v"(scale));
 
+  // scores X of the raw products S, plus PLUS (an expression in v)
+#define AMX_MASKED_SCORES(X, S, SMALL, PLUS)                                                                       \
+  if constexpr (!CAP) {                                                                                            \
+    _Pragma("unroll") for (int v = 0; v < 16; ++v) (X)[v] = __builtin_fmaf((S)[v], scale, PLUS);                   \
+  } else if (SMALL) {                                                                                              \
+    asm volatile("");                                                                                              \
+    _Pragma("unroll") for (int v = 0; v < 16; ++v) (X)[v] = capped_small((S)[v], w.scores, PLUS);                  \
+  } else {                                                                                                         \
+    asm volatile("");                                                                                              \
+    _Pragma("unroll") for (int v = 0; v < 16; ++v) (X)[v] = capped((S)[v], w.scores.in, w.scores.cap) + (PLUS);    \
+  }
   // one key tile from stage (CK, CV)
 #define AMX_MASKED_TILE(T, CK, CV)                                                                                 \
   if ((T) >= own_begin && (T) < own_end) {                                                                         \
@@ -148,25 +176,70 @@ __global__ __launch_bounds__(64 * kWaves) void attention_masked_kernel(const uin
       const bf16x8 a = *reinterpret_cast<const bf16x8*>((CK) + kb * kFragBytes + lane_off);                        \
       s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[kb], s, 0, 0, 0);                                          \
     }                                                                                                              \
-    float x[16];                                                                                                   \
+    float x[16], shift = 0.f;                                                                                      \
     const int key0 = (T) * 32 + row_in_tile;                                                                       \
-    const float away = (float)(nearest - key0);                                                                    \
-    _Pragma("unroll") for (int v = 0; v < 16; ++v) {                                                               \
-      x[v] = CAP ? capped(s[v], w.scores.in, w.scores.cap) : s[v] * w.scores.scale;                                \
-      if constexpr (SLOPE) x[v] = __builtin_fmaf(-slope, __builtin_fabsf(away - (float)(8 * (v >> 2) + (v & 3))), x[v]); \
+    bool small = false;                                                                                            \
+    if constexpr (CAP) {                                                                                           \
+      float size = __builtin_fabsf(s[0]);                                                                          \
+      _Pragma("unroll") for (int v = 1; v < 16; ++v) size = fmaxf(size, __builtin_fabsf(s[v]));                    \
+      small = __builtin_amdgcn_ballot_w64(size > w.scores.small) == 0; /* uniform */                               \
+    }                                                                                                              \
+    if (SLOPE && (T) * 32 + 31 <= all_nearest) { /* uniform: in front of the nearest keys */                       \
+      asm volatile("");                                                                                            \
+      AMX_MASKED_SCORES(x, s, small, step[v])                                                                      \
+      shift = slope * (float)(nearest - key0);                                                                     \
+    } else {                                                                                                       \
+      asm volatile("");                                                                                            \
+      AMX_MASKED_SCORES(x, s, small, 0.f)                                                                          \
+      if constexpr (SLOPE) {                                                                                       \
+        const float away = (float)(nearest - key0);                                                                \
+        _Pragma("unroll") for (int v = 0; v < 16; ++v)                                                             \
+          x[v] = __builtin_fmaf(-slope, __builtin_fabsf(away - (float)(8 * (v >> 2) + (v & 3))), x[v]);            \
+      }                                                                                                            \
     }                                                                                                              \
     if ((T) * 32 < all_from || (T) * 32 + 31 > all_to) { /* some key of the tile is not seen by some query */      \
+      asm volatile(""); /* (keeps the branch: most tiles skip the masking altogether) */                           \
       _Pragma("unroll") for (int v = 0; v < 16; ++v)                                                               \
-        if ((uint32_t)(key0 + 8 * (v >> 2) + (v & 3)) - (uint32_t)lo > span) x[v] = -__builtin_inff();                       \
+        if ((uint32_t)(key0 + 8 * (v >> 2) + (v & 3)) - (uint32_t)lo > span) x[v] = -__builtin_inff();             \
     }                                                                                                              \
     float mx = x[0];                                                                                               \
     _Pragma("unroll") for (int v = 1; v < 16; ++v) mx = fmaxf(mx, x[v]);                                           \
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));                                                                        \
-    const float m_raw = fmaxf(m, mx), m_new = m_raw == -__builtin_inff() ? 0.f : m_raw;                            \
-    const float alpha = m_raw == m ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);                                     \
-    AMX_ATTENTION_TILE_EXP(true, m, l, alpha)                                                                      \
+    const float own = mx - shift; /* the lane's largest score; the query's other keys are in lane ^ 32 */          \
+    const auto both = __builtin_amdgcn_permlane32_swap(f2u(own), f2u(own), false, false);                          \
+    const float top = fmaxf(u2f(both[0]), u2f(both[1])), m_new = fmaxf(m, top);                                    \
+    const float alpha = __builtin_amdgcn_exp2f(m - m_new), pmax = __builtin_amdgcn_exp2f(top - m_new);             \
+    /* what is subtracted from x. The score that holds the maximum gives exactly 0, whatever the shift rounds */   \
+    float base = m_new;                                                                                            \
+    if constexpr (SLOPE) base = own == m_new ? mx : m_new + shift;                                                 \
+    m = m_new;                                                                                                     \
+    /* The cast of the 32 weights of each query as one group, of which pmax is the largest. FP8 scales: the exponentials are of the    \
+       quotients, 2^(x - base - log2 S) (the rounding of base + log2 S is that of a score), and their sum takes S back.                \
+       A scale of 0 (all weights below 2^-17) casts them to 0. */                                                  \
     uint32_t pb[8];                                                                                                \
-    AMX_ATTENTION_TILE_CAST(x, pmax, pb, kPF16)                                                                    \
+    float sum = 0.f;                                                                                               \
+    if constexpr (SCALE_KIND == kScaleE5M2 || SCALE_KIND == kScaleE4M3) {                                          \
+      float S, R;                                                                                                  \
+      fp8_scale_inexact<SCALE_KIND>(pmax, S, R);                                                                   \
+      const float divide = S > 0.f ? S : 1.0f;                                                                     \
+      base += __builtin_amdgcn_logf(divide);                                                                       \
+      _Pragma("unroll") for (int v = 0; v < 16; ++v) x[v] = __builtin_amdgcn_exp2f(x[v] - base), sum += x[v];      \
+      sum *= divide;                                                                                               \
+      const _Float16 s_half = (_Float16)S; /* E5M2: exact, subnormals included */                                  \
+      _Pragma("unroll") for (int i = 0; i < 8; ++i) {                                                              \
+        const uint32_t code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(f2u(x[2 * i]), x[2 * i], x[2 * i + 1], 1.0f, 0); \
+        if constexpr (kPF16) {                                                                                     \
+          const f16x2 e = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(code, 256.0f, 0);                               \
+          pb[i] = __builtin_bit_cast(uint32_t, e * (f16x2){s_half, s_half});                                       \
+        } else {                                                                                                   \
+          const f32x2 e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 0);                                 \
+          pb[i] = __builtin_amdgcn_perm(f2u(e[1] * S), f2u(e[0] * S), 0x07060302u); /* exact: 6 significant bits */ \
+        }                                                                                                          \
+      }                                                                                                            \
+    } else {                                                                                                       \
+      _Pragma("unroll") for (int v = 0; v < 16; ++v) x[v] = __builtin_amdgcn_exp2f(x[v] - base), sum += x[v];      \
+      AMX_ATTENTION_TILE_CAST(x, pmax, pb, false)                                                                  \
+    }                                                                                                              \
+    l = __builtin_fmaf(l, alpha, sum);                                                                             \
     if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) { /* the maximum moved for some query: rescale */        \
       _Pragma("unroll") for (int db = 0; db < D / 32; ++db)                                                        \
         _Pragma("unroll") for (int v = 0; v < 16; ++v) o[db][v] *= alpha;                                          \
@@ -202,9 +275,12 @@ __global__ __launch_bounds__(64 * kWaves) void attention_masked_kernel(const uin
     }
   }
 #undef AMX_MASKED_TILE
+#undef AMX_MASKED_SCORES
 #undef AMX_MASKED_LOAD
 
   // out[query][h * D + d] = O^T[d][query] / l; register 4c + r of row block db is d = 32 db + 8 c + 4 (lane / 32) + r
+  const auto halves = __builtin_amdgcn_permlane32_swap(f2u(l), f2u(l), false, false);
+  l = u2f(halves[0]) + u2f(halves[1]);
   if (qw + (lane & 31) < w.Sq) {
     const float inv = l == 0.f ? 0.f : (kPF16 ? 0.03125f : 1.0f) / l;
     uint16_t* dst = out + ((int64_t)query * nheads + h) * D + row_in_tile;

@@ -7,12 +7,14 @@
 //     logprob = (y_t - m) - log S,   entropy = log S - T / S.
 // (Differences first and log2 e after them: the largest logit's is exactly 0, whatever its size.)
 //
+// A capped logit is x (1 + u P(u)), u = (x / cap)^2 (see scoring.h), up to 0.6 of the cap, which is most segments; in the others each value takes what
+// is its due. Logits of -inf have a path of their own too: there the differences are kept from 0 times infinity.
+//
 // Alternatives. A row is read in segments (4 chunks of 16 bytes to a lane, side by side over the wave); each leaves its largest logit
-// in LDS, each thread its own. The `top` best elements lie in the `top` best segments (by their largest, the earlier of equal
-// ones: every better segment holds an element that is better than all of a worse one's), and are not below the top-th largest of
-// the segments' or of the threads' maxima. So only those segments are read again, from the cache, and the few elements at or above that
-// bound are put in order by counting for each how many are better. Rows in which more than kList elements reach the bound
-// (equal logits by the hundred, fewer tokens than `top` not ruled out) take them one after the other.
+// in LDS, each thread keeps its own. The top-th largest of a wave's 64 and of the segments' bound the result from below, so only
+// segments that reach the bound are read again, from the cache, and the few elements at or above it are put in order by counting for
+// each how many are better. Rows in which more than kList elements reach the bound (equal logits by the hundred, fewer tokens than `top`
+// not ruled out) take them one after the other.
 #include "kernels.h"
 #include "scoring.h"
 
@@ -32,12 +34,40 @@ constexpr float kLn2 = 0.6931471805599453f;
 struct Sums {
   float m, s, t;
 };
-__device__ __forceinline__ Sums joined(Sums a, Sums b) {
-  const float m = fmaxf(a.m, b.m), to = m == -INFINITY ? 0.f : m;
-  // (nothing in one: sums of 0, or NaN; far below the other: 0 times a number)
-  const float da = a.m == -INFINITY ? 0.f : fmaxf(a.m - to, -1000.f), db = b.m == -INFINITY ? 0.f : fmaxf(b.m - to, -1000.f);
-  const float fa = __builtin_amdgcn_exp2f(da * kLog2e), fb = __builtin_amdgcn_exp2f(db * kLog2e);
-  return {m, a.s * fa + b.s * fb, (a.t + a.s * da) * fa + (b.t + b.s * db) * fb};
+
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) {
+  return u2f((uint32_t)__builtin_amdgcn_mov_dpp((int)f2u(v), CTRL, 0xF, 0xF, true));
+}
+// over the wave, in all lanes: quads, rows of 16, and the swaps of 16 and 32 lanes
+template <class Op>
+__device__ __forceinline__ float wave_reduce(float v, Op op) {
+  v = op(v, moved<0xB1>(v));
+  v = op(v, moved<0x4E>(v));
+  v = op(v, moved<0x124>(v));
+  v = op(v, moved<0x128>(v));
+  const auto a = __builtin_amdgcn_permlane16_swap(f2u(v), f2u(v), false, false);
+  v = op(u2f(a[0]), u2f(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(f2u(v), f2u(v), false, false);
+  return op(u2f(b[0]), u2f(b[1]));
+}
+__device__ __forceinline__ float wave_max(float v) { return wave_reduce(v, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float wave_min(float v) { return wave_reduce(v, [](float a, float b) { return fminf(a, b); }); }
+// (lanes add in orders of their own: the first one's sum, so that all go on with the same)
+__device__ __forceinline__ float wave_sum(float v) {
+  return u2f((uint32_t)__builtin_amdgcn_readfirstlane((int)f2u(wave_reduce(v, [](float a, float b) { return a + b; }))));
+}
+
+// sums against their own maximum, against the maximum `to`
+__device__ __forceinline__ Sums shifted(Sums a, float to) {
+  // (nothing in it: sums of 0, or NaN; far below: 0 times a number)
+  const float d = a.m == -INFINITY ? 0.f : fmaxf(a.m - to, -1000.f), f = __builtin_amdgcn_exp2f(d * kLog2e);
+  return {to, a.s * f, (a.t + a.s * d) * f};
+}
+__device__ __forceinline__ Sums wave_joined(Sums a) {
+  const float m = wave_max(a.m);
+  a = shifted(a, m);
+  return {m, wave_sum(a.s), wave_sum(a.t)};
 }
 
 __device__ __forceinline__ bool is_better(float v, int i, float w, int j) { return v > w || (v == w && i < j); }
@@ -49,35 +79,36 @@ struct LogprobWork {
   int32_t* top_ids;
   int64_t ld;
   int vocab, top, parts, per_part;  // per_part: segments
-  float in, cap;                    // as in Scores, the cap itself
+  float in, cap, inverse, small;    // in as in Scores; the cap, its inverse, and how far the polynomial goes
   float4* sums;                     // workspace: (m, S, T) of each row and part
   uint2* tops;                      // workspace: (logit, id) [row][part][top], best first
 };
 
+__device__ __forceinline__ float capped_small(const LogprobWork& w, float x) {
+  const float z = x * w.inverse, u = z * z;
+  const float p = __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, kTanh[3], kTanh[2]), kTanh[1]), kTanh[0]);
+  return x * __builtin_fmaf(u, p, 1.0f);
+}
 // A logit, capped; -inf stays.
 template <bool CAP>
 __device__ __forceinline__ float value_of(const LogprobWork& w, float x) {
-  if constexpr (CAP) return x == -INFINITY ? x : capped(x, w.in, w.cap);
-  return x;
+  if constexpr (!CAP) return x;
+  return x == -INFINITY ? x : __builtin_fabsf(x) <= w.small ? capped_small(w, x) : capped(x, w.in, w.cap);
 }
 
 struct Selection {
-  float best[kThreads];
   float list_v[kList];
   int list_i[kList];
   float wave_v[kWaves];
   int wave_i[kWaves];
   int count;
-  float bound;
 };
 
 // The k best of the elements that each(f) hands to this thread as f(logit, id), k in all threads together, in order: emit(rank, logit, id).
-// No element below `bound` is among them. What is not there (of rows with NaN) comes out as id -1.
+// No element below `bound` is among them. What is not there (of rows with NaN) comes out as id -1. l.count is 0.
 template <class Each, class Emit>
 __device__ __forceinline__ void select_best(Selection& l, int k, float bound, Each each, Emit emit) {
   const int t = threadIdx.x;
-  if (t == 0) l.count = 0;
-  __syncthreads();
   each([&](float v, int i) {
     if (v >= bound) {
       const int at = atomicAdd(&l.count, 1);
@@ -91,6 +122,7 @@ __device__ __forceinline__ void select_best(Selection& l, int k, float bound, Ea
       const float v = l.list_v[c];
       const int i = l.list_i[c];
       int rank = 0;
+#pragma unroll 8
       for (int o = 0; o < n; ++o) rank += is_better(l.list_v[o], l.list_i[o], v, i) ? 1 : 0;
       if (rank < k) emit(rank, v, i);
     }
@@ -122,21 +154,15 @@ __device__ __forceinline__ void select_best(Selection& l, int k, float bound, Ea
   }
 }
 
-// the k-th largest of n <= kThreads values (k <= n), one to a thread
-__device__ __forceinline__ float kth_largest(Selection& l, int n, int k, float mine) {
-  const int t = threadIdx.x;
-  l.best[t] = mine;
-  __syncthreads();
-  if (t < n) {
-    int rank = 0;
-    for (int o = 0; o < n; ++o) rank += is_better(l.best[o], o, mine, t) ? 1 : 0;
-    if (rank == k - 1) l.bound = mine;
-  }
-  __syncthreads();
-  return l.bound;
+// the k-th largest of a wave's values (k <= 64; none is NaN): the least of those that fewer than k exceed
+__device__ __forceinline__ float kth_of_wave(float mine, int k) {
+  int above = 0;
+#pragma unroll
+  for (int o = 0; o < 64; ++o) above += u2f((uint32_t)__builtin_amdgcn_readlane((int)f2u(mine), o)) > mine ? 1 : 0;
+  return wave_min(above < k ? mine : INFINITY);
 }
 
-// What is left to do for a row of which everything is known: thread 0.
+// What is left to do for a row of which everything is known: one thread.
 template <bool CAP>
 __device__ __forceinline__ void finish(const LogprobWork& w, int64_t row, Sums all, float log_s, float target) {
   const bool nothing = all.m == -INFINITY && all.s == 0.f;
@@ -159,7 +185,8 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(LogprobWork w)
   __shared__ Selection l;
   __shared__ Sums wave_sums[kWaves];
   __shared__ float segment_best[TOP ? kSegments : 1];
-  __shared__ int chosen[TOP ? kMostTop : 1];
+  __shared__ int chosen[TOP ? kSegments : 1], chosen_count;
+  __shared__ float bounds[2][kWaves];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int64_t row = blockIdx.x / (uint32_t)w.parts;
   const int part = (int)(blockIdx.x - (uint32_t)row * (uint32_t)w.parts);
@@ -191,50 +218,75 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(LogprobWork w)
           else
             v[c * kE + i] = u2f(word);
         }
-    } else {
+    } else {  // chunks that lie within the row still come whole
 #pragma unroll
-      for (int c = 0; c < kChunks; ++c)
+      for (int c = 0; c < kChunks; ++c) {
+        const int i = first + c * 64 * kE;
+        if (i >= 0 && i + kE <= w.vocab) {
+          const u32x4 r = *reinterpret_cast<const u32x4*>(x + i);
 #pragma unroll
-        for (int e = 0; e < kE; ++e) {
-          const int i = first + c * 64 * kE + e;
-          v[c * kE + e] = i >= 0 && i < w.vocab ? value(x[i]) : -INFINITY;
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t word = r[e];
+            if constexpr (BF16)
+              v[c * kE + 2 * e] = u2f(word << 16), v[c * kE + 2 * e + 1] = u2f(word & 0xFFFF0000u);
+            else
+              v[c * kE + e] = u2f(word);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < kE; ++e) v[c * kE + e] = i + e >= 0 && i + e < w.vocab ? value(x[i + e]) : -INFINITY;
         }
+      }
     }
   };
 
   // ---- the pass
+  if (t == 0) l.count = 0, chosen_count = 0;
   Sums mine = {-INFINITY, 0.f, 0.f};
   float best = -INFINITY;  // of the thread, as logits
   for (int s = s0 + wave; s < s1; s += kWaves) {
     float v[kN];
     load(s, v);
-    float most = v[0];
+    float most = v[0], edge = CAP ? __builtin_fabsf(v[0]) : v[0];  // edge: the largest size, or the smallest value
 #pragma unroll
-    for (int i = 1; i < kN; ++i) most = fmaxf(most, v[i]);
+    for (int i = 1; i < kN; ++i) {
+      most = fmaxf(most, v[i]);
+      edge = CAP ? fmaxf(edge, __builtin_fabsf(v[i])) : fminf(edge, v[i]);
+    }
     most = fmaxf(most, -INFINITY);  // (a NaN alone)
     if constexpr (TOP) {
       best = fmaxf(best, most);
-      float all = most;
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor(all, o, 64));
+      const float all = wave_max(most);
       if (lane == 0) segment_best[s - s0] = all;
     }
     const float m = fmaxf(mine.m, value_of<CAP>(w, most)), to = m == -INFINITY ? 0.f : m;
-    const float d = mine.m == -INFINITY ? 0.f : fmaxf(mine.m - to, -1000.f), f = __builtin_amdgcn_exp2f(d * kLog2e);
-    mine.t = (mine.t + mine.s * d) * f, mine.s *= f, mine.m = m;
+    mine = shifted(mine, to);
+    mine.m = m;
+    if (__builtin_amdgcn_ballot_w64(CAP ? edge > w.small : edge == -INFINITY) == 0) {  // uniform
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const float z = value_of<CAP>(w, v[i]) - to, e = __builtin_amdgcn_exp2f(z * kLog2e);
-      mine.s += e;
-      mine.t = __builtin_fmaf(e, fmaxf(z, -1000.f), mine.t);  // (0 times -inf)
+      for (int i = 0; i < kN; ++i) {
+        const float z = (CAP ? capped_small(w, v[i]) : v[i]) - to, e = __builtin_amdgcn_exp2f(z * kLog2e);
+        mine.s += e, mine.t = __builtin_fmaf(e, z, mine.t);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        const float z = value_of<CAP>(w, v[i]) - to, e = __builtin_amdgcn_exp2f(z * kLog2e);
+        mine.s += e, mine.t = __builtin_fmaf(e, fmaxf(z, -1000.f), mine.t);  // (0 times -inf)
+      }
     }
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1)
-    mine = joined(mine, Sums{__shfl_xor(mine.m, o, 64), __shfl_xor(mine.s, o, 64), __shfl_xor(mine.t, o, 64)});
-  if (lane == 0) wave_sums[wave] = mine;
+  mine = wave_joined(mine);
+  const float bound_here = TOP ? kth_of_wave(best, w.top) : 0.f;
+  if (lane == 0) wave_sums[wave] = mine, bounds[0][wave] = bound_here;
   __syncthreads();
-  const Sums all = joined(joined(wave_sums[0], wave_sums[1]), joined(wave_sums[2], wave_sums[3]));
+  const float m = fmaxf(fmaxf(wave_sums[0].m, wave_sums[1].m), fmaxf(wave_sums[2].m, wave_sums[3].m));
+  Sums all = {m, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    const Sums a = shifted(wave_sums[i], m);
+    all.s += a.s, all.t += a.t;
+  }
   const float log_s = kLn2 * __builtin_amdgcn_logf(all.s);
   if (t == 0) {
     if (w.parts == 1)
@@ -244,17 +296,25 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(LogprobWork w)
   }
   if constexpr (TOP) {
     const int segments = max(s1 - s0, 0), k = w.top;
-    if (t < kMostTop) chosen[t] = -1;
-    float bound = kth_largest(l, kThreads, k, best);
-    for (int s = t; s < segments; s += kThreads) {
-      const float v = segment_best[s];
-      int rank = 0;
-      for (int o = 0; o < segments; ++o) rank += is_better(segment_best[o], o, v, s) ? 1 : 0;
-      if (rank < k) chosen[rank] = s;
+    float bound = fmaxf(fmaxf(bounds[0][0], bounds[0][1]), fmaxf(bounds[0][2], bounds[0][3]));
+    if (segments >= k) {  // (uniform) the k-th largest of the segments' as well
+      float least = INFINITY;
+      for (int s = t; s < segments; s += kThreads) {
+        const float v = segment_best[s];
+        int above = 0;
+#pragma unroll 8
+        for (int o = 0; o < segments; ++o) above += segment_best[o] > v ? 1 : 0;
+        if (above < k) least = fminf(least, v);
+      }
+      least = wave_min(least);
+      if (lane == 0) bounds[1][wave] = least;
+      __syncthreads();
+      bound = fmaxf(bound, fminf(fminf(bounds[1][0], bounds[1][1]), fminf(bounds[1][2], bounds[1][3])));
     }
+    for (int s = t; s < segments; s += kThreads)
+      if (segment_best[s] >= bound) chosen[atomicAdd(&chosen_count, 1)] = s;
     __syncthreads();
-    if (segments >= k) bound = fmaxf(bound, segment_best[chosen[k - 1]]);
-    const int count = min(segments, k);
+    const int count = chosen_count;
     auto each = [&](auto f) {
       for (int c = wave; c < count; c += kWaves) {
         const int s = s0 + chosen[c];
@@ -282,45 +342,39 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(LogprobWork w)
 template <bool BF16, bool CAP, bool TOP>
 __global__ __launch_bounds__(kThreads) void token_logprobs_join_kernel(LogprobWork w) {
   __shared__ Selection l;
-  __shared__ Sums total;
-  const int t = threadIdx.x, k = w.top, parts = w.parts;
+  const int t = threadIdx.x, lane = t & 63, k = w.top, parts = w.parts;
   const int64_t row = blockIdx.x;
-  if (t < 64) {
-    Sums mine = {-INFINITY, 0.f, 0.f};
-    if (t < parts) {
-      const float4 v = w.sums[row * parts + t];
-      mine = {v.x, v.y, v.z};
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1)
-      mine = joined(mine, Sums{__shfl_xor(mine.m, o, 64), __shfl_xor(mine.s, o, 64), __shfl_xor(mine.t, o, 64)});
-    if (t == 0) {
-      float target = 0.f;
-      if (w.targets) {
-        const int at = w.targets[row];
-        if (at >= 0 && at < w.vocab) {
-          if constexpr (BF16)
-            target = u2f((uint32_t)static_cast<const uint16_t*>(w.logits)[row * w.ld + at] << 16);
-          else
-            target = static_cast<const float*>(w.logits)[row * w.ld + at];
-        }
-      }
-      finish<CAP>(w, row, mine, kLn2 * __builtin_amdgcn_logf(mine.s), target);
-      total = mine;
+  if (t == 0) l.count = 0;
+  float target = 0.f;
+  if (t == 0 && w.targets) {
+    const int at = w.targets[row];
+    if (at >= 0 && at < w.vocab) {
+      if constexpr (BF16)
+        target = u2f((uint32_t)static_cast<const uint16_t*>(w.logits)[row * w.ld + at] << 16);
+      else
+        target = static_cast<const float*>(w.logits)[row * w.ld + at];
     }
   }
+  // every wave for itself
+  Sums all = {-INFINITY, 0.f, 0.f};
+  if (lane < parts) {
+    const float4 v = w.sums[row * parts + lane];
+    all = {v.x, v.y, v.z};
+  }
+  const uint2* tops = w.tops + row * parts * k;
+  float bound = -INFINITY;
   if constexpr (TOP) {
-    // the parts' first `deep` elements are `top` or more: the top-th largest of them bounds the result
-    const uint2* tops = w.tops + row * parts * k;
-    const int deep = (k + parts - 1) / parts, n = deep * parts;
-    float head = -INFINITY;
-    if (t < n) {
-      const float v = u2f(tops[t / deep * k + t % deep].x);
-      head = v == v ? v : -INFINITY;
-    }
-    const float bound = kth_largest(l, n, k, head);
-    const Sums all = total;
-    const float log_s = kLn2 * __builtin_amdgcn_logf(all.s);
+    // A part's k-th bounds the result, and so does the k-th largest of the parts' first where there are so many (a NaN: none there)
+    float head = -INFINITY, tail = -INFINITY;
+    if (lane < parts) head = fmaxf(u2f(tops[lane * k].x), -INFINITY), tail = fmaxf(u2f(tops[lane * k + k - 1].x), -INFINITY);
+    bound = wave_max(tail);
+    if (parts >= k) bound = fmaxf(bound, kth_of_wave(head, k));
+  }
+  all = wave_joined(all);
+  const float log_s = kLn2 * __builtin_amdgcn_logf(all.s);
+  if (t == 0) finish<CAP>(w, row, all, log_s, target);
+  if constexpr (TOP) {
+    __syncthreads();
     auto each = [&](auto f) {
       for (int i = t; i < parts * k; i += kThreads) {
         const uint2 v = tops[i];
@@ -391,9 +445,9 @@ int amxfp4_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int64
   if (!aligned(logits, dtype == 1 ? 2 : 4) || !aligned(targets, 4) || !aligned(logprob, 4) || !aligned(entropy, 4) ||
       !aligned(top_logprobs, 4) || !aligned(top_ids, 4))
     return report_error(AMX_ERR_INVALID_ARG, "token_logprobs: pointers must be aligned to their elements");
-  LogprobWork w = {logits, targets, logprob, entropy, top_logprobs, top_ids, ld, (int)vocab, (int)top, 0, 0, 0.f, 0.f, nullptr, nullptr};
+  LogprobWork w = {logits, targets, logprob, entropy, top_logprobs, top_ids, ld, (int)vocab, (int)top, 0, 0, 0.f, 0.f, 0.f, 0.f, nullptr, nullptr};
   w.parts = parts_of(dtype, rows, vocab, w.per_part);
-  if (cap > 0.f) w.in = 2 * kLog2e / cap, w.cap = cap;
+  if (cap > 0.f) w.in = 2 * kLog2e / cap, w.cap = cap, w.inverse = 1.0f / cap, w.small = kSmall * cap;
   if (w.parts > 1) {
     if (!workspace || workspace_bytes < amxfp4_token_logprobs_workspace_bytes(dtype, rows, vocab, top) || !aligned(workspace, 256))
       return report_error(AMX_ERR_WORKSPACE, "token_logprobs: workspace missing, too small or not 256-byte aligned");
