@@ -31,6 +31,7 @@ constexpr int kWaves = 4, kQueries = 32 * kWaves;  // waves and queries of a wor
 struct MaskedWork {
   const int32_t *first, *last;
   int Sq, Sk, kv_group, causal, pos0;
+  int turn;  // query blocks to a turn of the workgroups over the compute units (0: blocks in descending order)
   Scores scores;
 };
 
@@ -45,18 +46,19 @@ __device__ __forceinline__ int wave_max(int v) {
   return __builtin_amdgcn_readfirstlane(v);
 }
 
-template <int SCALE_KIND, int D, bool CAP, bool SLOPE>
-__global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : 3) void attention_masked_kernel(const uint8_t* __restrict__ Q_codes, const uint8_t* __restrict__ Q_scales,
-                                                                     int asym, const uint16_t* __restrict__ Kp,
-                                                                     const uint16_t* __restrict__ Vp, uint16_t* __restrict__ out, MaskedWork w) {
+// NT: key tiles to a step, 1 or 2.
+template <int SCALE_KIND, int D, bool CAP, bool SLOPE, int NT>
+__global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void attention_masked_kernel(
+    const uint8_t* __restrict__ Q_codes, const uint8_t* __restrict__ Q_scales, int asym, const uint16_t* __restrict__ Kp,
+    const uint16_t* __restrict__ Vp, uint16_t* __restrict__ out, MaskedWork w) {
   // FP8-E5M2 scales: probabilities as FP16 times 2^8, V^T biased by 2^-3, the 2^5 taken out with the row sum at the end
   constexpr bool kPF16 = SCALE_KIND == kScaleE5M2;
-  constexpr int kFrags = D / 16;  // of K, and of V, in a key tile
-  // two stages of (K tile, V tile), separate arrays so that loads into one stage are known not to alias reads of the other
-  __shared__ __attribute__((aligned(1024))) uint8_t ldsK0[kFrags * kFragBytes];
-  __shared__ __attribute__((aligned(1024))) uint8_t ldsV0[kFrags * kFragBytes];
-  __shared__ __attribute__((aligned(1024))) uint8_t ldsK1[kFrags * kFragBytes];
-  __shared__ __attribute__((aligned(1024))) uint8_t ldsV1[kFrags * kFragBytes];
+  constexpr int kFrags = D / 16, kTileBytes = kFrags * kFragBytes;  // of K, and of V, in a key tile
+  // two stages of (K tiles, V tiles), separate arrays so that loads into one stage are known not to alias reads of the other
+  __shared__ __attribute__((aligned(1024))) uint8_t ldsK0[NT * kTileBytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t ldsV0[NT * kTileBytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t ldsK1[NT * kTileBytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t ldsV1[NT * kTileBytes];
   __shared__ int edges[2][kWaves];
 
   const int lane = threadIdx.x & 63;
@@ -66,7 +68,25 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : 3) void attention_masked
   const int nheads = (int)gridDim.x;
   const int h = (nheads & 7) == 0 ? (int)(blockIdx.x & 7) * (nheads >> 3) + (int)(blockIdx.x >> 3) : (int)blockIdx.x;
   const int g = h / w.kv_group;
-  const int qw = (int)(gridDim.y - 1 - blockIdx.y) * kQueries + wave * 32;
+  const int blocks = (int)gridDim.y;
+  int block = blocks - 1 - (int)blockIdx.y;
+  if (w.turn > 0) {  // uniform
+    const int b = min(lane, blocks - 1), row0 = b * kQueries, row1 = min(row0 + kQueries, w.Sq) - 1;
+    int a = 0, z = w.Sk - 1;
+    if (w.first) a = max(w.first[row0], 0);
+    if (w.last) z = min(w.last[row1], z);
+    if (w.causal) z = min(z, w.pos0 + row1);
+    const int length = lane < blocks ? max(z - a + 1, 0) : -1;
+    int rank = 0;
+    for (int o = 0; o < blocks; ++o) {
+      const int other = __builtin_amdgcn_readlane(length, o);
+      rank += other > length || (other == length && o > lane) ? 1 : 0;
+    }
+    const int turn = (int)blockIdx.y / w.turn, in_turn = (int)blockIdx.y - turn * w.turn, size = min(w.turn, blocks - turn * w.turn);
+    const int wanted = turn & 1 ? turn * w.turn + size - 1 - in_turn : (int)blockIdx.y;
+    block = (int)__builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < blocks && rank == wanted));
+  }
+  const int qw = block * kQueries + wave * 32;
   const int Skv = (w.Sk + 63) & ~63;  // the V panel's keys
 
   // ---- the keys that this lane's query sees: from lo on, span more; rows past Sq repeat the last one
@@ -97,15 +117,24 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : 3) void attention_masked
       const_cast<uint8_t*>(reinterpret_cast<const uint8_t*>(Vp) + g * frags_v * kFragBytes), 0, (int)(frags_v * kFragBytes), 0x00020000);
   const int lane_off = lane * 16;
 
-  // this wave's share of tile T into stage (DK, DV): every fourth fragment of K, and of V (fragment f: row block f / 2, k-step f % 2)
-#define AMX_MASKED_LOAD(T, DK, DV)                                                                                 \
-  _Pragma("unroll") for (int i = 0; i < kFrags / kWaves; ++i) {                                                    \
-    const int f = wave + kWaves * i;                                                                               \
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(Kr, (lds_ptr_t)((DK) + f * kFragBytes), 16, lane_off,                 \
-                                             ((T) * kFrags + f) * kFragBytes, 0, 0);                               \
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(Vr, (lds_ptr_t)((DV) + f * kFragBytes), 16, lane_off,                 \
-                                             ((f >> 1) * (Skv / 16) + (f & 1) + 2 * (T)) * kFragBytes, 0, 0);      \
-  }
+  // this wave's share of the tiles from `t` on into stage (K, V): every fourth fragment of either (fragment f of V: row block f / 2, k-step
+  // f % 2). Behind the last tile that one comes again.
+  auto load = [&](int t, uint8_t* K, uint8_t* V) __attribute__((always_inline)) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int tile = NT == 1 ? t : min(t + n, t_end - 1);
+#pragma unroll
+      for (int i = 0; i < kFrags / kWaves; ++i) {
+        const int f = wave + kWaves * i;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(Kr, (lds_ptr_t)(K + n * kTileBytes + f * kFragBytes), 16, lane_off,
+                                                 (tile * kFrags + f) * kFragBytes, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(Vr, (lds_ptr_t)(V + n * kTileBytes + f * kFragBytes), 16, lane_off,
+                                                 ((f >> 1) * (Skv / 16) + (f & 1) + 2 * tile) * kFragBytes, 0, 0);
+      }
+    }
+  };
+
+  if (t_begin < t_end) load(t_begin, ldsK0, ldsV0);
 
   // ---- this wave's 32 queries as the B operand of the first product, dequantized here from their codes
   bf16x8 qf[kFrags];
@@ -156,127 +185,187 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : 3) void attention_masked
   float scale = w.scores.scale;
   if constexpr (SLOPE && !CAP) asm volatile("" : "+v"(scale));
 
-  // scores X of the raw products S, plus PLUS (an expression in v)
-#define AMX_MASKED_SCORES(X, S, SMALL, PLUS)                                                                       \
-  if constexpr (!CAP) {                                                                                            \
-    _Pragma("unroll") for (int v = 0; v < 16; ++v) (X)[v] = __builtin_fmaf((S)[v], scale, PLUS);                   \
-  } else if (SMALL) {                                                                                              \
-    asm volatile("");                                                                                              \
-    _Pragma("unroll") for (int v = 0; v < 16; ++v) (X)[v] = capped_small((S)[v], w.scores, PLUS);                  \
-  } else {                                                                                                         \
-    asm volatile("");                                                                                              \
-    _Pragma("unroll") for (int v = 0; v < 16; ++v) (X)[v] = capped((S)[v], w.scores.in, w.scores.cap) + (PLUS);    \
-  }
-  // one key tile from stage (CK, CV)
-#define AMX_MASKED_TILE(T, CK, CV)                                                                                 \
-  if ((T) >= own_begin && (T) < own_end) {                                                                         \
-    f32x16 s;                                                                                                      \
-    _Pragma("unroll") for (int v = 0; v < 16; ++v) s[v] = 0.f;                                                     \
-    _Pragma("unroll") for (int kb = 0; kb < kFrags; ++kb) {                                                        \
-      const bf16x8 a = *reinterpret_cast<const bf16x8*>((CK) + kb * kFragBytes + lane_off);                        \
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[kb], s, 0, 0, 0);                                          \
-    }                                                                                                              \
-    float x[16], shift = 0.f;                                                                                      \
-    const int key0 = (T) * 32 + row_in_tile;                                                                       \
-    bool small = false;                                                                                            \
-    if constexpr (CAP) {                                                                                           \
-      float size = __builtin_fabsf(s[0]);                                                                          \
-      _Pragma("unroll") for (int v = 1; v < 16; ++v) size = fmaxf(size, __builtin_fabsf(s[v]));                    \
-      small = __builtin_amdgcn_ballot_w64(size > w.scores.small) == 0; /* uniform */                               \
-    }                                                                                                              \
-    if (SLOPE && (T) * 32 + 31 <= all_nearest) { /* uniform: in front of the nearest keys */                       \
-      asm volatile("");                                                                                            \
-      AMX_MASKED_SCORES(x, s, small, step[v])                                                                      \
-      shift = slope * (float)(nearest - key0);                                                                     \
-    } else {                                                                                                       \
-      asm volatile("");                                                                                            \
-      AMX_MASKED_SCORES(x, s, small, 0.f)                                                                          \
-      if constexpr (SLOPE) {                                                                                       \
-        const float away = (float)(nearest - key0);                                                                \
-        _Pragma("unroll") for (int v = 0; v < 16; ++v)                                                             \
-          x[v] = __builtin_fmaf(-slope, __builtin_fabsf(away - (float)(8 * (v >> 2) + (v & 3))), x[v]);            \
-      }                                                                                                            \
-    }                                                                                                              \
-    if ((T) * 32 < all_from || (T) * 32 + 31 > all_to) { /* some key of the tile is not seen by some query */      \
-      asm volatile(""); /* (keeps the branch: most tiles skip the masking altogether) */                           \
-      _Pragma("unroll") for (int v = 0; v < 16; ++v)                                                               \
-        if ((uint32_t)(key0 + 8 * (v >> 2) + (v & 3)) - (uint32_t)lo > span) x[v] = -__builtin_inff();             \
-    }                                                                                                              \
-    float mx = x[0];                                                                                               \
-    _Pragma("unroll") for (int v = 1; v < 16; ++v) mx = fmaxf(mx, x[v]);                                           \
-    const float own = mx - shift; /* the lane's largest score; the query's other keys are in lane ^ 32 */          \
-    const auto both = __builtin_amdgcn_permlane32_swap(f2u(own), f2u(own), false, false);                          \
-    const float top = fmaxf(u2f(both[0]), u2f(both[1])), m_new = fmaxf(m, top);                                    \
-    const float alpha = __builtin_amdgcn_exp2f(m - m_new), pmax = __builtin_amdgcn_exp2f(top - m_new);             \
-    /* what is subtracted from x. The score that holds the maximum gives exactly 0, whatever the shift rounds */   \
-    float base = m_new;                                                                                            \
-    if constexpr (SLOPE) base = own == m_new ? mx : m_new + shift;                                                 \
-    m = m_new;                                                                                                     \
-    /* The cast of the 32 weights of each query as one group, of which pmax is the largest. FP8 scales: the exponentials are of the    \
-       quotients, 2^(x - base - log2 S) (the rounding of base + log2 S is that of a score), and their sum takes S back.                \
-       A scale of 0 (all weights below 2^-17) casts them to 0. */                                                  \
-    uint32_t pb[8];                                                                                                \
-    float sum = 0.f;                                                                                               \
-    if constexpr (SCALE_KIND == kScaleE5M2 || SCALE_KIND == kScaleE4M3) {                                          \
-      float S, R;                                                                                                  \
-      fp8_scale_inexact<SCALE_KIND>(pmax, S, R);                                                                   \
-      const float divide = S > 0.f ? S : 1.0f;                                                                     \
-      base += __builtin_amdgcn_logf(divide);                                                                       \
-      _Pragma("unroll") for (int v = 0; v < 16; ++v) x[v] = __builtin_amdgcn_exp2f(x[v] - base), sum += x[v];      \
-      sum *= divide;                                                                                               \
-      const _Float16 s_half = (_Float16)S; /* E5M2: exact, subnormals included */                                  \
-      _Pragma("unroll") for (int i = 0; i < 8; ++i) {                                                              \
-        const uint32_t code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(f2u(x[2 * i]), x[2 * i], x[2 * i + 1], 1.0f, 0); \
-        if constexpr (kPF16) {                                                                                     \
-          const f16x2 e = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(code, 256.0f, 0);                               \
-          pb[i] = __builtin_bit_cast(uint32_t, e * (f16x2){s_half, s_half});                                       \
-        } else {                                                                                                   \
-          const f32x2 e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 0);                                 \
-          pb[i] = __builtin_amdgcn_perm(f2u(e[1] * S), f2u(e[0] * S), 0x07060302u); /* exact: 6 significant bits */ \
-        }                                                                                                          \
-      }                                                                                                            \
-    } else {                                                                                                       \
-      _Pragma("unroll") for (int v = 0; v < 16; ++v) x[v] = __builtin_amdgcn_exp2f(x[v] - base), sum += x[v];      \
-      AMX_ATTENTION_TILE_CAST(x, pmax, pb, false)                                                                  \
-    }                                                                                                              \
-    l = __builtin_fmaf(l, alpha, sum);                                                                             \
-    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) { /* the maximum moved for some query: rescale */        \
-      _Pragma("unroll") for (int db = 0; db < D / 32; ++db)                                                        \
-        _Pragma("unroll") for (int v = 0; v < 16; ++v) o[db][v] *= alpha;                                          \
-    }                                                                                                              \
-    _Pragma("unroll") for (int j = 0; j < 2; ++j) {                                                                \
-      const u32x4 b = {pb[4 * j], pb[4 * j + 1], pb[4 * j + 2], pb[4 * j + 3]};                                    \
-      _Pragma("unroll") for (int db = 0; db < D / 32; ++db) {                                                      \
-        const u32x4 a = *reinterpret_cast<const u32x4*>((CV) + (db * 2 + j) * kFragBytes + lane_off);              \
-        if constexpr (kPF16)                                                                                       \
-          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), \
-                                                         o[db], 0, 0, 0);                                          \
-        else                                                                                                       \
-          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),                           \
-                                                          __builtin_bit_cast(bf16x8, b), o[db], 0, 0, 0);          \
-      }                                                                                                            \
-    }                                                                                                              \
-  }
+  // Scores of a tile's raw products, each plus plus(v). (The empty statements keep the branches, here and below: without them both sides are
+  // computed and selected from.)
+  auto scores = [&](const f32x16& s, bool small, float (&x)[16], auto plus) __attribute__((always_inline)) {
+    if constexpr (!CAP) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) x[v] = __builtin_fmaf(s[v], scale, plus(v));
+    } else if (small) {
+      asm volatile("");
+#pragma unroll
+      for (int v = 0; v < 16; ++v) x[v] = capped_small(s[v], w.scores, plus(v));
+    } else {
+      asm volatile("");
+#pragma unroll
+      for (int v = 0; v < 16; ++v) x[v] = capped(s[v], w.scores.in, w.scores.cap) + plus(v);
+    }
+  };
 
-  if (t_begin < t_end) AMX_MASKED_LOAD(t_begin, ldsK0, ldsV0);
+  // NT key tiles from `t` on, out of stage (K, V)
+  auto step_of = [&](int t, const uint8_t* K, const uint8_t* V) __attribute__((always_inline)) {
+    if (t + NT <= own_begin || t >= own_end) return;
+    f32x16 s[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[n][v] = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < kFrags; ++kb)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const bf16x8 a = *reinterpret_cast<const bf16x8*>(K + n * kTileBytes + kb * kFragBytes + lane_off);
+        s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[kb], s[n], 0, 0, 0);
+      }
+    const bool all_seen = t * 32 >= all_from && (t + NT) * 32 - 1 <= all_to;  // every key of the tiles, by every query (uniform)
+    bool small[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      small[n] = false;
+      if constexpr (CAP) {
+        float size = __builtin_fabsf(s[n][0]);
+#pragma unroll
+        for (int v = 1; v < 16; ++v) size = fmaxf(size, __builtin_fabsf(s[n][v]));
+        small[n] = __builtin_amdgcn_ballot_w64(size > w.scores.small) == 0;
+      }
+    }
+    // ---- the lane's largest score of each tile, the query's (its other keys are in lane ^ 32), and the running maxima. own: what is
+    // subtracted from a score for it (the one that holds the maximum gives exactly 0, whatever the shift rounds)
+    float x[NT][16], base[NT], alpha[NT], pmax[NT];
+    auto maxima = [&](int n, float own, float shift) __attribute__((always_inline)) {
+      const auto both = __builtin_amdgcn_permlane32_swap(f2u(own - shift), f2u(own - shift), false, false);
+      const float top = fmaxf(u2f(both[0]), u2f(both[1])), m_new = fmaxf(m, top);
+      alpha[n] = __builtin_amdgcn_exp2f(m - m_new), pmax[n] = __builtin_amdgcn_exp2f(top - m_new);
+      base[n] = !SLOPE ? m_new : own - shift == m_new ? own : m_new + shift;
+      m = m_new;
+    };
+    // The scale of the cast, as a divisor: FP8 scales take the exponentials of the quotients, 2^(x - base - log2 S) (the rounding of base +
+    // log2 S is that of a score), and their sum takes S back. A scale of 0 (all weights below 2^-17) casts them to 0.
+    float S[NT], divide[NT];
+    auto scale_of_cast = [&](int n) __attribute__((always_inline)) {
+      if constexpr (SCALE_KIND == kScaleE5M2 || SCALE_KIND == kScaleE4M3) {
+        float inverse;
+        fp8_scale_inexact<SCALE_KIND>(pmax[n], S[n], inverse);
+        divide[n] = S[n] > 0.f ? S[n] : 1.0f;
+        base[n] += __builtin_amdgcn_logf(divide[n]);
+      } else {
+        float inverse;
+        (void)encode_scale_sr<SCALE_KIND>(pmax[n], S[n], inverse);
+        divide[n] = 1.0f;
+      }
+    };
+    if (!SLOPE && all_seen) {  // scores rise with the products: the largest of those first, then each less its base in one go
+      asm volatile("");
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float most = s[n][0];
+#pragma unroll
+        for (int v = 1; v < 16; ++v) most = fmaxf(most, s[n][v]);
+        float top = most * scale;
+        if constexpr (CAP) top = small[n] ? capped_small(most, w.scores, 0.f) : capped(most, w.scores.in, w.scores.cap);
+        maxima(n, top, 0.f);
+        scale_of_cast(n);
+        const float less = -base[n];
+        scores(s[n], small[n], x[n], [&](int) { return less; });
+      }
+    } else {
+      asm volatile("");
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const int key0 = (t + n) * 32 + row_in_tile;
+        float shift = 0.f;
+        if (SLOPE && (t + n) * 32 + 31 <= all_nearest) {  // uniform: in front of the nearest keys
+          asm volatile("");
+          scores(s[n], small[n], x[n], [&](int v) { return step[v]; });
+          shift = slope * (float)(nearest - key0);
+        } else {
+          asm volatile("");
+          scores(s[n], small[n], x[n], [](int) { return 0.f; });
+          if constexpr (SLOPE) {
+            const float away = (float)(nearest - key0);
+#pragma unroll
+            for (int v = 0; v < 16; ++v) x[n][v] = __builtin_fmaf(-slope, __builtin_fabsf(away - (float)(8 * (v >> 2) + (v & 3))), x[n][v]);
+          }
+        }
+        if (!all_seen) {
+          asm volatile("");
+#pragma unroll
+          for (int v = 0; v < 16; ++v)
+            if ((uint32_t)(key0 + 8 * (v >> 2) + (v & 3)) - (uint32_t)lo > span) x[n][v] = -__builtin_inff();
+        }
+        float own = x[n][0];
+#pragma unroll
+        for (int v = 1; v < 16; ++v) own = fmaxf(own, x[n][v]);
+        maxima(n, own, shift);
+        scale_of_cast(n);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) x[n][v] -= base[n];
+      }
+    }
+    // ---- the weights, their sum and their cast, 32 of a query as one group
+    uint32_t pb[NT][8];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float sum = 0.f;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) x[n][v] = __builtin_amdgcn_exp2f(x[n][v]), sum += x[n][v];
+      l = __builtin_fmaf(l, alpha[n], sum * divide[n]);
+      const _Float16 s_half = (_Float16)S[n];  // (E5M2: exact, subnormals included)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float a = x[n][2 * i], b = x[n][2 * i + 1];
+        if constexpr (SCALE_KIND == kScaleE5M2) {
+          const uint32_t code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(f2u(a), a, b, 1.0f, 0);
+          pb[n][i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(code, 256.0f, 0) * (f16x2){s_half, s_half});
+        } else if constexpr (SCALE_KIND == kScaleE4M3) {
+          const uint32_t code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(f2u(a), a, b, 1.0f, 0);
+          const f32x2 e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 0);
+          pb[n][i] = __builtin_amdgcn_perm(f2u(e[1] * S[n]), f2u(e[0] * S[n]), 0x07060302u);  // exact: 6 significant bits
+        } else {  // the conversions apply a power of two themselves (its exponent field: the first divides, the second multiplies)
+          const uint32_t code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(f2u(a), a, b, S[n], 0);
+          pb[n][i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, S[n], 0));
+        }
+      }
+    }
+    // ---- O^T
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      if (__builtin_amdgcn_ballot_w64(alpha[n] != 1.0f) != 0) {  // the maximum moved for some query: rescale
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) o[db][v] *= alpha[n];
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const u32x4 b = {pb[n][4 * j], pb[n][4 * j + 1], pb[n][4 * j + 2], pb[n][4 * j + 3]};
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) {
+          const u32x4 a = *reinterpret_cast<const u32x4*>(V + n * kTileBytes + (db * 2 + j) * kFragBytes + lane_off);
+          if constexpr (kPF16)
+            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), o[db], 0, 0, 0);
+          else
+            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), o[db], 0, 0, 0);
+        }
+      }
+    }
+  };
+
   AMX_WAIT_VMCNT(0);
   AMX_BARRIER();
-  for (int t = t_begin; t < t_end; t += 2) {
-    // stage 1 was last read during tile t - 1; the barrier that ended it lets every wave refill it now
-    if (t + 1 < t_end) AMX_MASKED_LOAD(t + 1, ldsK1, ldsV1);
-    AMX_MASKED_TILE(t, ldsK0, ldsV0);
+  for (int t = t_begin; t < t_end; t += 2 * NT) {
+    // stage 1 was last read in the step before; the barrier that ended it lets every wave refill it now
+    if (t + NT < t_end) load(t + NT, ldsK1, ldsV1);
+    step_of(t, ldsK0, ldsV0);
     AMX_WAIT_VMCNT(0);
     AMX_BARRIER();
-    if (t + 1 < t_end) {  // uniform over the workgroup
-      if (t + 2 < t_end) AMX_MASKED_LOAD(t + 2, ldsK0, ldsV0);
-      AMX_MASKED_TILE(t + 1, ldsK1, ldsV1);
+    if (t + NT < t_end) {  // uniform over the workgroup
+      if (t + 2 * NT < t_end) load(t + 2 * NT, ldsK0, ldsV0);
+      step_of(t + NT, ldsK1, ldsV1);
       AMX_WAIT_VMCNT(0);
       AMX_BARRIER();
     }
   }
-#undef AMX_MASKED_TILE
-#undef AMX_MASKED_SCORES
-#undef AMX_MASKED_LOAD
 
   // out[query][h * D + d] = O^T[d][query] / l; register 4c + r of row block db is d = 32 db + 8 c + 4 (lane / 32) + r
   const auto halves = __builtin_amdgcn_permlane32_swap(f2u(l), f2u(l), false, false);
@@ -292,6 +381,9 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : 3) void attention_masked
             pack_bf16(o[db][4 * c] * inv, o[db][4 * c + 1] * inv), pack_bf16(o[db][4 * c + 2] * inv, o[db][4 * c + 3] * inv));
   }
 }
+
+constexpr int64_t kMostOrdered = 768;
+constexpr int64_t kMostOfPairs = 512;  // workgroups of a launch whose waves take two key tiles to a step
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
@@ -334,11 +426,18 @@ extern "C" int amxfp4_attention_masked(const amx_format_t* fmt, int64_t q_heads,
   uint16_t* Vp = Kp + kv_heads * Sk * head_dim;
   hipError_t e = launch_expand_kv(fmt->scale, asym, K_codes, K_scales, Kp, V_codes, V_scales, Vp, Sk, head_dim, kv_heads, s);
   if (e != hipSuccess) return report_hip_error(e, "attention_masked: expansion launch");
-  const MaskedWork w = {first, last, (int)Sq, (int)Sk, (int)(q_heads / kv_heads), causal, (int)pos0, scores_of(scores, scale)};
+  MaskedWork w = {first, last, (int)Sq, (int)Sk, (int)(q_heads / kv_heads), causal, (int)pos0, 0, scores_of(scores, scale)};
   const dim3 grid((unsigned)q_heads, (unsigned)((Sq + kQueries - 1) / kQueries));
+  const int64_t workgroups = (int64_t)grid.x * grid.y;
+  if (workgroups > 256 && workgroups <= kMostOrdered && grid.y > 1 && grid.y <= 64) w.turn = q_heads < 256 ? (int)(256 / q_heads) : 1;
+  const bool pairs = workgroups <= kMostOfPairs;
   auto go = [&]<int SK, int D, bool CAP, bool SLOPE>() {
-    hipLaunchKernelGGL((attention_masked_kernel<SK, D, CAP, SLOPE>), grid, dim3(64 * kWaves), 0, s, Q_codes, Q_scales, asym ? 1 : 0,
-                       Kp, Vp, static_cast<uint16_t*>(out_bf16), w);
+    if (pairs)
+      hipLaunchKernelGGL((attention_masked_kernel<SK, D, CAP, SLOPE, 2>), grid, dim3(64 * kWaves), 0, s, Q_codes, Q_scales, asym ? 1 : 0,
+                         Kp, Vp, static_cast<uint16_t*>(out_bf16), w);
+    else
+      hipLaunchKernelGGL((attention_masked_kernel<SK, D, CAP, SLOPE, 1>), grid, dim3(64 * kWaves), 0, s, Q_codes, Q_scales, asym ? 1 : 0,
+                         Kp, Vp, static_cast<uint16_t*>(out_bf16), w);
   };
   auto with_scores = [&]<int SK, int D>() {
     if (w.scores.cap > 0.f)

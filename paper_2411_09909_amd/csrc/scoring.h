@@ -12,7 +12,7 @@ struct Scores {
   float in, cap;        // tanh(scale q.k / C) of a raw product s is 1 - 2 / (1 + exp2(s * in)); cap: C log2(e). 0: not capped
   float scale;          // softmax scale times log2(e)
   float small;          // raw products up to here may take the polynomial below (0: none)
-  float k1, k2, k3, k4;  // scale s (1 + k1' s^2 + ..): multiplied by the scale here
+  float k1, k2, k3;     // scale s (1 + k1' s^2 + ..): multiplied by the scale here
   const float* slopes;  // of the query heads, or nullptr
 };
 
@@ -24,9 +24,9 @@ inline bool scores_valid(const amx_scores_t* s) {
   return s->cap == 0.f || (s->cap >= 0x1p-20f && s->cap <= 0x1p20f);
 }
 
-// tanh z = z (1 + u (c1 + u (c2 + u (c3 + u c4)))), u = z^2, for |z| <= 0.6: coefficients fitted here for the least absolute error, 2.8e-8.
-// Six instructions at the full rate where the formula with exp2 and a reciprocal takes five, two of them at a quarter of it.
-constexpr float kSmall = 0.6f, kTanh[4] = {-0.33332247f, 0.13308099f, -0.051994339f, 0.015319208f};
+// tanh z = z (1 + u (c1 + u (c2 + u c3))), u = z^2, for |z| <= 0.45: coefficients fitted here for the least absolute error, 2^-23.6.
+// Five instructions at the full rate where the formula with exp2 and a reciprocal takes five, two of them at a quarter of it.
+constexpr float kSmall = 0.45f, kTanh[3] = {-0.33329531f, 0.13233127f, -0.045875340f};
 
 inline Scores scores_of(const amx_scores_t* s, float scale) {
   Scores r = {};
@@ -36,11 +36,11 @@ inline Scores scores_of(const amx_scores_t* s, float scale) {
     r.in = c * (2 * kLog2e), r.cap = s->cap * kLog2e;
     // as far as the powers of c stay in range: with a wide cap fewer terms up to a smaller size, with a very narrow one none
     if (c < 0x1p12f && scale < 0x1p20f) {
-      const int terms = c > 0x1p-12f ? 4 : c > 0x1p-30f ? 2 : 1;
-      r.small = (terms == 4 ? kSmall : terms == 2 ? 0.02f : 0x1p-12f) / c;
+      const int terms = c > 0x1p-12f ? 3 : c > 0x1p-30f ? 2 : 1;
+      r.small = (terms == 3 ? kSmall : terms == 2 ? 0.02f : 0x1p-12f) / c;
       r.k1 = r.scale * u * kTanh[0];
       if (terms >= 2) r.k2 = r.scale * u * u * kTanh[1];
-      if (terms == 4) r.k3 = r.scale * u * u * u * kTanh[2], r.k4 = r.scale * u * u * u * u * kTanh[3];
+      if (terms == 3) r.k3 = r.scale * u * u * u * kTanh[2];
     }
   }
   return r;
@@ -56,7 +56,7 @@ __device__ __forceinline__ float capped(float s, float in, float cap) {
 // The same of a product of at most Scores::small, plus a number.
 __device__ __forceinline__ float capped_small(float s, const Scores& w, float plus) {
   const float u = s * s;
-  const float p = __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, w.k4, w.k3), w.k2), w.k1), w.scale);
+  const float p = __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, w.k3, w.k2), w.k1), w.scale);
   return __builtin_fmaf(s, p, plus);
 }
 

@@ -7,7 +7,7 @@
 //     logprob = (y_t - m) - log S,   entropy = log S - T / S.
 // (Differences first and log2 e after them: the largest logit's is exactly 0, whatever its size.)
 //
-// A capped logit is x (1 + u P(u)), u = (x / cap)^2 (see scoring.h), up to 0.6 of the cap, which is most segments; in the others each value takes what
+// A capped logit is x (1 + u P(u)), u = (x / cap)^2, up to 0.6 of the cap, which is most segments; in the others each value takes what
 // is its due. Logits of -inf have a path of their own too: there the differences are kept from 0 times infinity.
 //
 // Alternatives. A row is read in segments (4 chunks of 16 bytes to a lane, side by side over the wave); each leaves its largest logit
@@ -30,6 +30,9 @@ constexpr int kList = 512;      // candidates that are put in order at once
 constexpr int kMostTop = 64;
 constexpr int kMostParts = 64;
 constexpr float kLn2 = 0.6931471805599453f;
+// P: fitted here for the least absolute error of tanh z = z (1 + u P(u)) for |z| <= 0.6, 2.8e-8 (one term more than in scoring.h: logits are
+// answers themselves)
+constexpr float kWide = 0.6f, kP[4] = {-0.33332247f, 0.13308099f, -0.051994339f, 0.015319208f};
 
 struct Sums {
   float m, s, t;
@@ -86,7 +89,7 @@ struct LogprobWork {
 
 __device__ __forceinline__ float capped_small(const LogprobWork& w, float x) {
   const float z = x * w.inverse, u = z * z;
-  const float p = __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, kTanh[3], kTanh[2]), kTanh[1]), kTanh[0]);
+  const float p = __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, kP[3], kP[2]), kP[1]), kP[0]);
   return x * __builtin_fmaf(u, p, 1.0f);
 }
 // A logit, capped; -inf stays.
@@ -447,7 +450,7 @@ int amxfp4_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int64
     return report_error(AMX_ERR_INVALID_ARG, "token_logprobs: pointers must be aligned to their elements");
   LogprobWork w = {logits, targets, logprob, entropy, top_logprobs, top_ids, ld, (int)vocab, (int)top, 0, 0, 0.f, 0.f, 0.f, 0.f, nullptr, nullptr};
   w.parts = parts_of(dtype, rows, vocab, w.per_part);
-  if (cap > 0.f) w.in = 2 * kLog2e / cap, w.cap = cap, w.inverse = 1.0f / cap, w.small = kSmall * cap;
+  if (cap > 0.f) w.in = 2 * kLog2e / cap, w.cap = cap, w.inverse = 1.0f / cap, w.small = kWide * cap;
   if (w.parts > 1) {
     if (!workspace || workspace_bytes < amxfp4_token_logprobs_workspace_bytes(dtype, rows, vocab, top) || !aligned(workspace, 256))
       return report_error(AMX_ERR_WORKSPACE, "token_logprobs: workspace missing, too small or not 256-byte aligned");
