@@ -49,16 +49,21 @@ typedef struct {
  *   windows     first[i] = p - window + 1, causal.
  *   padding     rows: last[i] = -1. Keys behind the last that any row sees are not looked at (Sk is rounded up to 32 by what the
  *               caller likes).
- *   fmt, heads, Sq, Sk, head_dim, codes, scales, scale, workspace: as amxfp4_attention (groups of 32, heads of 128 or 64, Sk a
- *               multiple of 32, Sq and Sk at most 2^20; amxfp4_attention_workspace_bytes()). Sq may exceed Sk. Scales of V that are
+ *   fmt, heads, Sq, Sk, head_dim, codes, scales, scale: as amxfp4_attention (groups of 32, heads of 128 or 64, Sk a multiple of 32, Sq
+ *               and Sk at most 2^20). Sq may exceed Sk. Scales of V that are
  *               not finite make all rows of a workgroup (128 neighbouring ones) that walks over them undefined, also those that do not see
  *               them; scales of K only the rows that see them.
  *   scores      HOST, or NULL for neither.
  *   causal      0 or 1; 0 <= pos0 <= 2^30.
  *   first, last device int32 [Sq], any values, 4-byte aligned, or NULL.
  *   out_bf16    device out, [Sq][q_heads * head_dim] BF16 bit patterns, 16-byte aligned.
- * The same call gives the same bits.
+ *   workspace   at least amxfp4_attention_masked_workspace_bytes() bytes (which are more than amxfp4_attention's), 256-byte aligned
+ *               (AMX_ERR_WORKSPACE otherwise).
+ * The same call gives the same bits. (Few rows against many keys are split over the keys: each range's maxima first, so that every tile is
+ * cast against the running maximum of all keys before it, as without the split.)
  */
+size_t amxfp4_attention_masked_workspace_bytes(const amx_format_t* fmt, int64_t q_heads, int64_t kv_heads, int64_t Sq, int64_t Sk,
+                                               int64_t head_dim);
 int amxfp4_attention_masked(const amx_format_t* fmt, int64_t q_heads, int64_t kv_heads, int64_t Sq, int64_t Sk, int64_t head_dim,
                             const uint8_t* Q_codes, const uint8_t* Q_scales, const uint8_t* K_codes, const uint8_t* K_scales,
                             const uint8_t* V_codes, const uint8_t* V_scales, float scale, const amx_scores_t* scores, int32_t causal,

@@ -125,6 +125,8 @@ def _load():
     L.amxfp4_attention_masked.argtypes = [fp, i64, i64, i64, i64, i64, vp, vp, vp, vp, vp, vp, f32, sp, i32, i64, vp, vp, vp, vp,
                                           ctypes.c_size_t, vp]
     L.amxfp4_attention_masked.restype = ctypes.c_int
+    L.amxfp4_attention_masked_workspace_bytes.argtypes = [fp, i64, i64, i64, i64, i64]
+    L.amxfp4_attention_masked_workspace_bytes.restype = ctypes.c_size_t
     L.amxfp4_paged_attention_scored.argtypes = [fp, ctypes.POINTER(AmxPagedPool), vp, i64, i64, vp, i64, i64, vp, vp, vp, f32, sp, i64, vp, vp,
                                                 ctypes.c_size_t, vp]
     L.amxfp4_paged_attention_scored.restype = ctypes.c_int
@@ -875,6 +877,10 @@ def _scores(cap, slopes, q_heads):
     return ctypes.byref(AmxScores(float(cap), 0, None if slopes is None else slopes.data_ptr()))
 
 
+def attention_masked_workspace_bytes(fmt, q_heads, kv_heads, Sq, Sk, head_dim=128):
+    return int(load().amxfp4_attention_masked_workspace_bytes(ctypes.byref(fmt), q_heads, kv_heads, Sq, Sk, head_dim))
+
+
 def attention_masked(fmt, q_codes, q_scales, k_codes, k_scales, v_codes, v_scales, scale, causal=True, pos0=0, first=None, last=None,
                      cap=0.0, slopes=None, out=None, workspace=None):
     """amxfp4_attention_masked: attention(.., merged=True) whose query row i, at position pos0 + i, sees the keys from first[i] to
@@ -900,7 +906,8 @@ def attention_masked(fmt, q_codes, q_scales, k_codes, k_scales, v_codes, v_scale
     if out is None:
         out = torch.empty((Sq, q_heads * D), dtype=torch.bfloat16, device=q_codes.device)
     if workspace is None:
-        workspace = torch.empty(max(256, attention_workspace_bytes(fmt, q_heads, kv_heads, Sq, Sk, D)), dtype=torch.uint8, device=q_codes.device)
+        workspace = torch.empty(max(256, attention_masked_workspace_bytes(fmt, q_heads, kv_heads, Sq, Sk, D)), dtype=torch.uint8,
+                                device=q_codes.device)
     _here(out, workspace)
     if out.dtype != torch.bfloat16 or out.numel() != Sq * q_heads * D:
         raise AmxError("attention_masked: out must be bfloat16 [%d, %d]" % (Sq, q_heads * D))

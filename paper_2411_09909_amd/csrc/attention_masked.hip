@@ -25,12 +25,15 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {  // (what is not a number stays so)
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
 }
+constexpr float kLowest = -0x1.fffffep127f;
 constexpr int kWaves = 4, kQueries = 32 * kWaves;  // waves and queries of a workgroup
 
 // What one launch reads beside the operands.
 struct MaskedWork {
   const int32_t *first, *last;
   int Sq, Sk, kv_group, causal, pos0;
+  float *maxima, *parts;  // of split rows: [head][row][chunk]; [head][chunk][row][D]
+  float2* ends;           // [head][chunk][row]: maximum and sum
   int turn;  // query blocks to a turn of the workgroups over the compute units (0: blocks in descending order)
   Scores scores;
 };
@@ -46,8 +49,9 @@ __device__ __forceinline__ int wave_max(int v) {
   return __builtin_amdgcn_readfirstlane(v);
 }
 
-// NT: key tiles to a step, 1 or 2.
-template <int SCALE_KIND, int D, bool CAP, bool SLOPE, int NT>
+// NT: key tiles to a step, 1 or 2. PASS: kWhole, or a chunk of a workgroup's key tiles (see kMaxima).
+enum { kWhole, kMaxima, kPart };
+template <int SCALE_KIND, int D, bool CAP, bool SLOPE, int NT, int PASS>
 __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void attention_masked_kernel(
     const uint8_t* __restrict__ Q_codes, const uint8_t* __restrict__ Q_scales, int asym, const uint16_t* __restrict__ Kp,
     const uint16_t* __restrict__ Vp, uint16_t* __restrict__ out, MaskedWork w) {
@@ -56,9 +60,9 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
   constexpr int kFrags = D / 16, kTileBytes = kFrags * kFragBytes;  // of K, and of V, in a key tile
   // two stages of (K tiles, V tiles), separate arrays so that loads into one stage are known not to alias reads of the other
   __shared__ __attribute__((aligned(1024))) uint8_t ldsK0[NT * kTileBytes];
-  __shared__ __attribute__((aligned(1024))) uint8_t ldsV0[NT * kTileBytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t ldsV0[PASS == kMaxima ? 1 : NT * kTileBytes];
   __shared__ __attribute__((aligned(1024))) uint8_t ldsK1[NT * kTileBytes];
-  __shared__ __attribute__((aligned(1024))) uint8_t ldsV1[NT * kTileBytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t ldsV1[PASS == kMaxima ? 1 : NT * kTileBytes];
   __shared__ int edges[2][kWaves];
 
   const int lane = threadIdx.x & 63;
@@ -106,9 +110,17 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
   const int least = min(min(edges[0][0], edges[0][1]), min(edges[0][2], edges[0][3]));
   const int most = max(max(edges[1][0], edges[1][1]), max(edges[1][2], edges[1][3]));
   // key tiles that the workgroup loads, and that this wave computes (uniform)
-  const int t_begin = most < 0 ? 0 : __builtin_amdgcn_readfirstlane(least >> 5);
-  const int t_end = most < 0 ? 0 : __builtin_amdgcn_readfirstlane((most >> 5) + 1);
-  const int own_begin = to < 0 ? 0 : from >> 5, own_end = to < 0 ? 0 : (to >> 5) + 1;
+  int t_begin = most < 0 ? 0 : __builtin_amdgcn_readfirstlane(least >> 5);
+  int t_end = most < 0 ? 0 : __builtin_amdgcn_readfirstlane((most >> 5) + 1);
+  int own_begin = to < 0 ? 0 : from >> 5, own_end = to < 0 ? 0 : (to >> 5) + 1;
+  const int chunk = (int)blockIdx.z, chunks = (int)gridDim.z;
+  if constexpr (PASS != kWhole) {
+    // (whole steps: what a step has beyond the block's last tile is masked, what it had beyond a chunk's would not be)
+    static_assert(NT == 2, "chunks of pairs");
+    const int steps = (t_end - t_begin + 1) / 2;
+    t_end = min(t_end, t_begin + 2 * (steps * (chunk + 1) / chunks)), t_begin += 2 * (steps * chunk / chunks);
+    own_begin = max(own_begin, t_begin), own_end = min(own_end, t_end);
+  }
 
   const int64_t frags_k = (int64_t)(w.Sk / 32) * kFrags, frags_v = (int64_t)(D / 32) * (Skv / 16);
   const __amdgpu_buffer_rsrc_t Kr = __builtin_amdgcn_make_buffer_rsrc(
@@ -128,8 +140,9 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
         const int f = wave + kWaves * i;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(Kr, (lds_ptr_t)(K + n * kTileBytes + f * kFragBytes), 16, lane_off,
                                                  (tile * kFrags + f) * kFragBytes, 0, 0);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(Vr, (lds_ptr_t)(V + n * kTileBytes + f * kFragBytes), 16, lane_off,
-                                                 ((f >> 1) * (Skv / 16) + (f & 1) + 2 * tile) * kFragBytes, 0, 0);
+        if constexpr (PASS != kMaxima)
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(Vr, (lds_ptr_t)(V + n * kTileBytes + f * kFragBytes), 16, lane_off,
+                                                   ((f >> 1) * (Skv / 16) + (f & 1) + 2 * tile) * kFragBytes, 0, 0);
       }
     }
   };
@@ -164,7 +177,9 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
     for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
   // Running maximum (in units of log2) and sum of this lane's query; the sum of the keys that this lane has, until the end. The maximum
   // starts finite: a query that has seen no key yet then has weights of 0 and a factor of 1 without any test.
-  float m = -0x1.fffffep127f, l = 0.f;
+  float m = kLowest, l = 0.f;
+  if constexpr (PASS == kPart)
+    for (int c = 0; c < chunk; ++c) m = fmaxf(m, w.maxima[((int64_t)h * w.Sq + query) * chunks + c]);
   const int row_in_tile = 4 * (lane >> 5);    // key of register v: 8 (v / 4) + row_in_tile + v % 4
   // Distances are taken from the nearest key that the query sees: all its scores shift alike, and stay small where it sees far keys
   // only. In a tile in front of all the wave's nearest keys a score is f(q.k) + slope (key in the tile) - slope (distance of the tile's first
@@ -218,21 +233,23 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
         s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[kb], s[n], 0, 0, 0);
       }
     const bool all_seen = t * 32 >= all_from && (t + NT) * 32 - 1 <= all_to;  // every key of the tiles, by every query (uniform)
-    bool small[NT];
+    bool small = false;
+    if constexpr (CAP) {
+      float size = __builtin_fabsf(s[0][0]);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      small[n] = false;
-      if constexpr (CAP) {
-        float size = __builtin_fabsf(s[n][0]);
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int v = 1; v < 16; ++v) size = fmaxf(size, __builtin_fabsf(s[n][v]));
-        small[n] = __builtin_amdgcn_ballot_w64(size > w.scores.small) == 0;
-      }
+        for (int v = 0; v < 16; ++v) size = fmaxf(size, __builtin_fabsf(s[n][v]));
+      small = __builtin_amdgcn_ballot_w64(size > w.scores.small) == 0;
     }
     // ---- the lane's largest score of each tile, the query's (its other keys are in lane ^ 32), and the running maxima. own: what is
     // subtracted from a score for it (the one that holds the maximum gives exactly 0, whatever the shift rounds)
     float x[NT][16], base[NT], alpha[NT], pmax[NT];
     auto maxima = [&](int n, float own, float shift) __attribute__((always_inline)) {
+      if constexpr (PASS == kMaxima) {
+        m = fmaxf(m, own - shift);
+        return;
+      }
       const auto both = __builtin_amdgcn_permlane32_swap(f2u(own - shift), f2u(own - shift), false, false);
       const float top = fmaxf(u2f(both[0]), u2f(both[1])), m_new = fmaxf(m, top);
       alpha[n] = __builtin_amdgcn_exp2f(m - m_new), pmax[n] = __builtin_amdgcn_exp2f(top - m_new);
@@ -262,11 +279,12 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
 #pragma unroll
         for (int v = 1; v < 16; ++v) most = fmaxf(most, s[n][v]);
         float top = most * scale;
-        if constexpr (CAP) top = small[n] ? capped_small(most, w.scores, 0.f) : capped(most, w.scores.in, w.scores.cap);
+        if constexpr (CAP) top = small ? capped_small(most, w.scores, 0.f) : capped(most, w.scores.in, w.scores.cap);
         maxima(n, top, 0.f);
+        if constexpr (PASS == kMaxima) continue;
         scale_of_cast(n);
         const float less = -base[n];
-        scores(s[n], small[n], x[n], [&](int) { return less; });
+        scores(s[n], small, x[n], [&](int) { return less; });
       }
     } else {
       asm volatile("");
@@ -276,11 +294,11 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
         float shift = 0.f;
         if (SLOPE && (t + n) * 32 + 31 <= all_nearest) {  // uniform: in front of the nearest keys
           asm volatile("");
-          scores(s[n], small[n], x[n], [&](int v) { return step[v]; });
+          scores(s[n], small, x[n], [&](int v) { return step[v]; });
           shift = slope * (float)(nearest - key0);
         } else {
           asm volatile("");
-          scores(s[n], small[n], x[n], [](int) { return 0.f; });
+          scores(s[n], small, x[n], [](int) { return 0.f; });
           if constexpr (SLOPE) {
             const float away = (float)(nearest - key0);
 #pragma unroll
@@ -297,11 +315,13 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
 #pragma unroll
         for (int v = 1; v < 16; ++v) own = fmaxf(own, x[n][v]);
         maxima(n, own, shift);
+        if constexpr (PASS == kMaxima) continue;
         scale_of_cast(n);
 #pragma unroll
         for (int v = 0; v < 16; ++v) x[n][v] -= base[n];
       }
     }
+    if constexpr (PASS == kMaxima) return;
     // ---- the weights, their sum and their cast, 32 of a query as one group
     uint32_t pb[NT][8];
 #pragma unroll
@@ -367,10 +387,26 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
     }
   }
 
+  const bool stored = qw + (lane & 31) < w.Sq;
+  if constexpr (PASS == kMaxima) {
+    const auto both = __builtin_amdgcn_permlane32_swap(f2u(m), f2u(m), false, false);
+    if (stored && lane < 32) w.maxima[((int64_t)h * w.Sq + query) * chunks + chunk] = fmaxf(u2f(both[0]), u2f(both[1]));
+    return;
+  }
   // out[query][h * D + d] = O^T[d][query] / l; register 4c + r of row block db is d = 32 db + 8 c + 4 (lane / 32) + r
   const auto halves = __builtin_amdgcn_permlane32_swap(f2u(l), f2u(l), false, false);
   l = u2f(halves[0]) + u2f(halves[1]);
-  if (qw + (lane & 31) < w.Sq) {
+  if (!stored) return;
+  if constexpr (PASS == kPart) {
+    const int64_t row = ((int64_t)h * chunks + chunk) * w.Sq + query;
+    if (lane < 32) w.ends[row] = make_float2(m, l);
+    float* dst = w.parts + row * D + row_in_tile;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<float4*>(dst + db * 32 + c * 8) = make_float4(o[db][4 * c], o[db][4 * c + 1], o[db][4 * c + 2], o[db][4 * c + 3]);
+  } else {
     const float inv = l == 0.f ? 0.f : (kPF16 ? 0.03125f : 1.0f) / l;
     uint16_t* dst = out + ((int64_t)query * nheads + h) * D + row_in_tile;
 #pragma unroll
@@ -382,7 +418,47 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
   }
 }
 
+// The chunks' sums against their own maxima, of which the last one's is the row's: a thread to four dimensions of a row and head.
+template <int D>
+__global__ __launch_bounds__(256) void attention_masked_join_kernel(const float* __restrict__ parts, const float2* __restrict__ ends,
+                                                                    uint16_t* __restrict__ out, int Sq, int heads, int chunks, float bias) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, at = i / (D / 4);
+  if (at >= (int64_t)Sq * heads) return;
+  const int h = (int)(at / Sq), row = (int)(at - (int64_t)h * Sq), d = (int)(i % (D / 4)) * 4;
+  const int64_t first = (int64_t)h * chunks * Sq + row;
+  const float top = ends[first + (int64_t)(chunks - 1) * Sq].x;
+  float4 sum = make_float4(0, 0, 0, 0);
+  float l = 0.f;
+#pragma unroll 4
+  for (int c = 0; c < chunks; ++c) {
+    const int64_t r = first + (int64_t)c * Sq;
+    const float2 end = ends[r];
+    const float f = __builtin_amdgcn_exp2f(end.x - top);
+    const float4 v = *reinterpret_cast<const float4*>(parts + r * D + d);
+    sum.x += v.x * f, sum.y += v.y * f, sum.z += v.z * f, sum.w += v.w * f, l += end.y * f;
+  }
+  const float inv = l == 0.f ? 0.f : bias / l;
+  *reinterpret_cast<uint2*>(out + ((int64_t)row * heads + h) * D + d) = make_uint2(pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv));
+}
+
 constexpr int64_t kMostOrdered = 768;
+constexpr int64_t kSplitBelow = 256, kSplitInto = 768, kLeastOfChunk = 8, kMostChunks = 32;
+
+// Chunks that the key tiles of a block of queries are cut into.
+int chunks_of(int64_t Hq, int64_t Sq, int64_t tiles) {
+  const int64_t workgroups = Hq * ((Sq + kQueries - 1) / kQueries);
+  if (workgroups > kSplitBelow) return 1;
+  int64_t c = (kSplitInto + workgroups - 1) / workgroups;
+  if (c > tiles / kLeastOfChunk) c = tiles / kLeastOfChunk;
+  return (int)(c > kMostChunks ? kMostChunks : c < 2 ? 1 : c);
+}
+
+size_t panels_bytes(int64_t Hq, int64_t Hkv, int64_t Sq, int64_t Sk, int64_t D) { return (attention_workspace_bytes(Hq, Hkv, Sq, Sk, D) + 255) & ~(size_t)255; }
+size_t rows_bytes(int64_t Hq, int64_t Sq, int chunks, int64_t floats) { return ((size_t)(Hq * Sq * chunks * floats) * sizeof(float) + 255) & ~(size_t)255; }
+size_t workspace_bytes_of(int64_t Hq, int64_t Hkv, int64_t Sq, int64_t Sk, int64_t D) {
+  const int c = chunks_of(Hq, Sq, Sk / 32);
+  return panels_bytes(Hq, Hkv, Sq, Sk, D) + (c == 1 ? 0 : rows_bytes(Hq, Sq, c, 1) + rows_bytes(Hq, Sq, c, 2) + rows_bytes(Hq, Sq, c, D));
+}
 constexpr int64_t kMostOfPairs = 512;  // workgroups of a launch whose waves take two key tiles to a step
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -392,7 +468,17 @@ bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) &
 
 using namespace amx;
 
-extern "C" int amxfp4_attention_masked(const amx_format_t* fmt, int64_t q_heads, int64_t kv_heads, int64_t Sq, int64_t Sk,
+extern "C" {
+
+size_t amxfp4_attention_masked_workspace_bytes(const amx_format_t* fmt, int64_t q_heads, int64_t kv_heads, int64_t Sq, int64_t Sk,
+                                               int64_t head_dim) {
+  if (!fmt || q_heads <= 0 || kv_heads <= 0 || q_heads % kv_heads || q_heads > 65535 || Sq <= 0 || Sk <= 0 || Sk % 32 || Sq > (1 << 20) ||
+      Sk > (1 << 20) || (head_dim != 128 && head_dim != 64))
+    return 0;
+  return workspace_bytes_of(q_heads, kv_heads, Sq, Sk, head_dim);
+}
+
+int amxfp4_attention_masked(const amx_format_t* fmt, int64_t q_heads, int64_t kv_heads, int64_t Sq, int64_t Sk,
                                        int64_t head_dim, const uint8_t* Q_codes, const uint8_t* Q_scales, const uint8_t* K_codes,
                                        const uint8_t* K_scales, const uint8_t* V_codes, const uint8_t* V_scales, float scale,
                                        const amx_scores_t* scores, int32_t causal, int64_t pos0, const int32_t* first,
@@ -417,7 +503,7 @@ extern "C" int amxfp4_attention_masked(const amx_format_t* fmt, int64_t q_heads,
   if (!aligned(Q_codes, 16) || !aligned(K_codes, 16) || !aligned(V_codes, 16) || !aligned(Q_scales, 2) || !aligned(K_scales, 2) ||
       !aligned(V_scales, 2) || !aligned(out_bf16, 16) || !aligned(first, 4) || !aligned(last, 4))
     return report_error(AMX_ERR_INVALID_ARG, "attention_masked: codes and out need 16-byte, scales 2-byte, first and last 4-byte alignment");
-  if (!workspace || workspace_bytes < attention_workspace_bytes(q_heads, kv_heads, Sq, Sk, head_dim) || !aligned(workspace, 256))
+  if (!workspace || workspace_bytes < workspace_bytes_of(q_heads, kv_heads, Sq, Sk, head_dim) || !aligned(workspace, 256))
     return report_error(AMX_ERR_WORKSPACE, "attention_masked: workspace missing, too small or not 256-byte aligned");
 
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
@@ -426,18 +512,39 @@ extern "C" int amxfp4_attention_masked(const amx_format_t* fmt, int64_t q_heads,
   uint16_t* Vp = Kp + kv_heads * Sk * head_dim;
   hipError_t e = launch_expand_kv(fmt->scale, asym, K_codes, K_scales, Kp, V_codes, V_scales, Vp, Sk, head_dim, kv_heads, s);
   if (e != hipSuccess) return report_hip_error(e, "attention_masked: expansion launch");
-  MaskedWork w = {first, last, (int)Sq, (int)Sk, (int)(q_heads / kv_heads), causal, (int)pos0, 0, scores_of(scores, scale)};
-  const dim3 grid((unsigned)q_heads, (unsigned)((Sq + kQueries - 1) / kQueries));
+  MaskedWork w = {};
+  w.first = first, w.last = last, w.Sq = (int)Sq, w.Sk = (int)Sk, w.kv_group = (int)(q_heads / kv_heads), w.causal = causal, w.pos0 = (int)pos0;
+  w.scores = scores_of(scores, scale);
+  uint16_t* out = static_cast<uint16_t*>(out_bf16);
+  // (keys behind the last row's position are not seen: no more chunks than there is room for)
+  const int64_t keys = causal && pos0 + Sq < Sk ? pos0 + Sq : Sk;
+  const int chunks = chunks_of(q_heads, Sq, (keys + 31) / 32);
+  dim3 grid((unsigned)q_heads, (unsigned)((Sq + kQueries - 1) / kQueries));
   const int64_t workgroups = (int64_t)grid.x * grid.y;
   if (workgroups > 256 && workgroups <= kMostOrdered && grid.y > 1 && grid.y <= 64) w.turn = q_heads < 256 ? (int)(256 / q_heads) : 1;
   const bool pairs = workgroups <= kMostOfPairs;
+  if (chunks > 1) {
+    uint8_t* at = static_cast<uint8_t*>(workspace) + panels_bytes(q_heads, kv_heads, Sq, Sk, head_dim);
+    w.maxima = reinterpret_cast<float*>(at);
+    w.ends = reinterpret_cast<float2*>(at += rows_bytes(q_heads, Sq, chunks, 1));
+    w.parts = reinterpret_cast<float*>(at += rows_bytes(q_heads, Sq, chunks, 2));
+  }
   auto go = [&]<int SK, int D, bool CAP, bool SLOPE>() {
-    if (pairs)
-      hipLaunchKernelGGL((attention_masked_kernel<SK, D, CAP, SLOPE, 2>), grid, dim3(64 * kWaves), 0, s, Q_codes, Q_scales, asym ? 1 : 0,
-                         Kp, Vp, static_cast<uint16_t*>(out_bf16), w);
-    else
-      hipLaunchKernelGGL((attention_masked_kernel<SK, D, CAP, SLOPE, 1>), grid, dim3(64 * kWaves), 0, s, Q_codes, Q_scales, asym ? 1 : 0,
-                         Kp, Vp, static_cast<uint16_t*>(out_bf16), w);
+    auto pass = [&]<int NT, int PASS>() {
+      hipLaunchKernelGGL((attention_masked_kernel<SK, D, CAP, SLOPE, NT, PASS>), grid, dim3(64 * kWaves), 0, s, Q_codes, Q_scales,
+                         asym ? 1 : 0, Kp, Vp, out, w);
+    };
+    if (chunks > 1) {
+      grid.z = (unsigned)chunks;
+      pass.template operator()<2, kMaxima>();
+      pass.template operator()<2, kPart>();
+      hipLaunchKernelGGL((attention_masked_join_kernel<D>), dim3((unsigned)((Sq * q_heads * (D / 4) + 255) / 256)), dim3(256), 0, s, w.parts, w.ends,
+                         out, (int)Sq, (int)q_heads, chunks, SK == kScaleE5M2 ? 0.03125f : 1.0f);
+    } else if (pairs) {
+      pass.template operator()<2, kWhole>();
+    } else {
+      pass.template operator()<1, kWhole>();
+    }
   };
   auto with_scores = [&]<int SK, int D>() {
     if (w.scores.cap > 0.f)
@@ -455,3 +562,5 @@ extern "C" int amxfp4_attention_masked(const amx_format_t* fmt, int64_t q_heads,
   e = hipGetLastError();
   return e == hipSuccess ? AMX_OK : report_hip_error(e, "attention_masked launch");
 }
+
+}  // extern "C"

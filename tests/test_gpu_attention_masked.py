@@ -34,7 +34,7 @@ def check(Hq, Hkv, Sq, Sk, D, kind=ref.FP8_E5M2, asym=1, causal=True, pos0=0, fi
     q, k, v = heads(Hq, Sq, seed, gain, D), heads(Hkv, Sk, seed + 1, d=D), heads(Hkv, Sk, seed + 2, d=D)
     want, allowed = scoring_ref.masked_attention(q, k, v, D ** -0.5, causal, pos0, first, last, cap, slopes, kind, asym, rows)
     fmt, ops = operands(q, k, v, kind, asym)
-    need = binding.attention_workspace_bytes(fmt, Hq, Hkv, Sq, Sk, D)
+    need = binding.attention_masked_workspace_bytes(fmt, Hq, Hkv, Sq, Sk, D)
     ws = torch.full((need + 1024,), 0xFF, dtype=torch.uint8, device="cuda")
     out = torch.full((Sq + 2, Hq * D), 7.0, dtype=torch.bfloat16, device="cuda")
     how = dict(causal=causal, pos0=pos0, first=ints(first), last=ints(last), cap=cap, slopes=None if slopes is None else torch.from_numpy(slopes).cuda())
@@ -116,6 +116,29 @@ def test_many_tiles(D, kind, asym):
     check(2, 1, S, S, D, kind, asym, rows=at, first=first, last=last, causal=False, seed=7)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kind,asym", FORMATS)
+@pytest.mark.parametrize("cap,sloped", [(0.0, False), (20.0, False), (0.0, True), (3.0, True)])
+def test_few_rows_are_split_over_the_keys(kind, asym, D, cap, sloped):
+    check(2, 1, 5, 1024, D, kind, asym, pos0=1010, cap=cap, slopes=slopes_of(2) if sloped else None)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Sq,Sk,pos0", [(1, 512, 500), (3, 544, 541), (40, 1504, 1460), (130, 768, 600), (33, 4096, 4063)])
+@pytest.mark.parametrize("mask", ["causal", "window", "all", "some", "near the end"])
+def test_masks_of_split_rows(mask, Sq, Sk, pos0, D):
+    """Chunks that no row sees, ranges that end within one, rows that see nothing, a maximum in the first chunk."""
+    i, rng = pos0 + np.arange(Sq), np.random.RandomState(Sq)
+    how = dict(causal=(mask in ("causal", "window", "near the end")))
+    if mask == "window":
+        how["first"] = i - 299
+    elif mask == "some":
+        how["first"], how["last"] = rng.randint(-9, Sk, Sq), np.where(rng.rand(Sq) < 0.3, -1, rng.randint(0, Sk + 9, Sq))
+    elif mask == "near the end":
+        how["first"] = np.full(Sq, pos0 - 3)
+    check(2, 1, Sq, Sk, D, pos0=pos0, cap=30.0, rows=sorted(set(rng.randint(0, Sq, 12).tolist() + [0, Sq - 1])), **how)
+
+
 def test_scales_that_are_not_finite_stay_where_they_are():
     """Keys that nobody sees may hold any scale; a key's that some rows see spoils those rows alone."""
     Hq, Sq, Sk, D = 2, 96, 160, 128
@@ -132,12 +155,12 @@ def test_scales_that_are_not_finite_stay_where_they_are():
     assert torch.equal(got[40:], want[40:]) and torch.isnan(got[:40].float()).all()
 
 
-def test_another_stream_a_graph_and_calls_at_the_same_time():
-    Sq = Sk = 320
-    first = ints(documents([100, 220])[0])
+@pytest.mark.parametrize("Sq,Sk", [(320, 320), (20, 1024)])
+def test_another_stream_a_graph_and_calls_at_the_same_time(Sq, Sk):
+    first = ints(documents([100, 220])[0][:Sq])
     fmt, ops = operands(heads(8, Sq, 1), heads(2, Sk, 2), heads(2, Sk, 3), ref.FP8_E5M2, 1)
     slopes = torch.from_numpy(slopes_of(8)).cuda()
-    call = lambda **kw: binding.attention_masked(fmt, *ops, 0.1, first=first, cap=30.0, slopes=slopes, **kw)  # noqa: E731
+    call = lambda **kw: binding.attention_masked(fmt, *ops, 0.1, pos0=Sk - Sq, first=first, cap=30.0, slopes=slopes, **kw)  # noqa: E731
     want = call()
     streams = [torch.cuda.Stream() for _ in range(2)]
     outs = []
@@ -147,7 +170,7 @@ def test_another_stream_a_graph_and_calls_at_the_same_time():
             outs.append(call())
     torch.cuda.synchronize()
     assert all(torch.equal(o, want) for o in outs)
-    out, ws = torch.zeros_like(want), torch.empty(binding.attention_workspace_bytes(fmt, 8, 2, Sq, Sk, 128), dtype=torch.uint8, device="cuda")
+    out, ws = torch.zeros_like(want), torch.empty(binding.attention_masked_workspace_bytes(fmt, 8, 2, Sq, Sk, 128), dtype=torch.uint8, device="cuda")
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         call(out=out, workspace=ws)

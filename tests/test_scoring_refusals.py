@@ -39,8 +39,10 @@ def test_attention_masked(lib):
         assert call(D=D) == -2
     for kw in BAD_SCORES:
         assert call(sc=scores(**kw)) == -1, kw
-    need = binding.attention_workspace_bytes(fmt(), 8, 2, 40, 64, 128)
-    assert need > 0
+    need = binding.attention_masked_workspace_bytes(fmt(), 8, 2, 40, 64, 128)
+    assert need > 0 and binding.attention_masked_workspace_bytes(fmt(), 8, 3, 40, 64, 128) == 0 and binding.attention_masked_workspace_bytes(fmt(), 8, 2, 40, 65, 128) == 0
+    few = binding.attention_masked_workspace_bytes(fmt(), 8, 2, 40, 4096, 128)
+    assert few > binding.attention_workspace_bytes(fmt(), 8, 2, 40, 4096, 128) and call(Sk=4096, size=few - 1) == -3
     for kw in (dict(ws=None), dict(size=need - 1), dict(ws=ctypes.c_void_p(0x1080))):
         assert call(**kw) == -3, kw
     assert b"workspace" in lib.amxfp4_last_error()
