@@ -837,8 +837,9 @@ def paged_attention(fmt, q, pool, table, lens, starts, positions, scale, max_key
     and positions out of paged_plan()). max_keys: at least the longest sequence, 0 if not known. Returns BF16 [rows, q_heads *
     head_dim]; rows behind the last sequence's are left as they were (zeros in a new tensor). cap, slopes: amxfp4_paged_attention_scored, as for
     attention_masked()."""
-    if out is not None and workspace is not None and not cap and slopes is None:
-        rc = (_calls or _bound()).paged_attention(fmt, q, pool, table, lens, starts, positions, float(scale), max_keys, out, workspace)
+    if out is not None and workspace is not None:
+        more = (float(cap), slopes) if cap or slopes is not None else ()
+        rc = (_calls or _bound()).paged_attention(fmt, q, pool, table, lens, starts, positions, float(scale), max_keys, out, workspace, *more)
         if rc is not None:
             return out if rc == 0 else _check(rc)
     p = _pool(fmt, pool)
@@ -888,6 +889,10 @@ def attention_masked(fmt, q_codes, q_scales, k_codes, k_scales, v_codes, v_scale
     [q_heads]: they fall by slopes[h] for each key of distance. Operands as for attention() (contiguous). Returns BF16 [Sq, q_heads * head_dim];
     rows that see nothing are zeros."""
     operands = (q_codes, q_scales, k_codes, k_scales, v_codes, v_scales)
+    if out is not None and workspace is not None:
+        rc = (_calls or _bound()).attention_masked(fmt, *operands, float(scale), bool(causal), pos0, first, last, float(cap), slopes, out, workspace)
+        if rc is not None:
+            return out if rc == 0 else _check(rc)
     _here(*operands)
     if any(t.dtype != torch.uint8 for t in operands) or any(t.dim() != 3 for t in operands[::2]):
         raise AmxError("attention_masked: uint8 operands, codes of three dimensions")
@@ -934,6 +939,11 @@ def token_logprobs(logits, targets=None, top=0, cap=0.0, out=None, workspace=Non
     """amxfp4_token_logprobs: float32 or BF16 logits [rows, vocab] (rows any distance apart) -> TokenLogprobs: the log probability of each
     row's target (int32 [rows]; 0 for one outside the vocabulary), the row's entropy, and the log probabilities and ids of its `top` largest
     logits. cap > 0: logits x become cap tanh(x / cap) first. out: the buffers of a TokenLogprobs, float32 and int32."""
+    if out is not None and workspace is not None:
+        out = out if type(out) is TokenLogprobs else TokenLogprobs(*out)
+        rc = (_calls or _bound()).token_logprobs(logits, targets, top, float(cap), out, workspace)
+        if rc is not None:
+            return out if rc == 0 else _check(rc)
     _need_cuda(logits)
     if logits.dtype not in (torch.float32, torch.bfloat16) or logits.dim() != 2 or (logits.stride(1) != 1 and logits.shape[1] > 1):
         raise AmxError("token_logprobs: float32 or bfloat16 logits [rows, vocab] with contiguous rows")
@@ -945,7 +955,7 @@ def token_logprobs(logits, targets=None, top=0, cap=0.0, out=None, workspace=Non
         f = lambda *shape: torch.empty(shape, dtype=torch.float32, device=logits.device)  # noqa: E731
         out = (None if targets is None else f(rows), f(rows)) + (
             (f(rows, top), torch.empty((rows, top), dtype=torch.int32, device=logits.device)) if top else (None, None))
-    out = TokenLogprobs(*out)
+    out = out if type(out) is TokenLogprobs else TokenLogprobs(*out)
     for t, dtype, shape in zip(out, (torch.float32,) * 3 + (torch.int32,), ((rows,), (rows,), (rows, top), (rows, top))):
         if t is not None:
             _here(t)

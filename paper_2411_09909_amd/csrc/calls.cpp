@@ -11,6 +11,7 @@
 
 #include "../../include/amxfp4.h"
 #include "../../include/amxfp4_paged.h"
+#include "../../include/amxfp4_scoring.h"
 
 namespace {
 
@@ -30,11 +31,15 @@ struct {
   decltype(&amxfp4_paged_write) paged_write;
   decltype(&amxfp4_paged_read) paged_read;
   decltype(&amxfp4_paged_attention) paged_attention;
+  decltype(&amxfp4_paged_attention_scored) paged_attention_scored;
+  decltype(&amxfp4_attention_masked) attention_masked;
+  decltype(&amxfp4_token_logprobs) token_logprobs;
 } entry;
 constexpr const char* kEntries[] = {"amxfp4_quantize", "amxfp4_quantize_scaled", "amxfp4_quantize_batched", "amxfp4_tensor_scale",
                                     "amxfp4_gemm", "amxfp4_gemm_scaled", "amxfp4_gemm_prepared", "amxfp4_attention",
                                     "amxfp4_attention_merged", "amxfp4_attention_decode", "amxfp4_paged_plan", "amxfp4_paged_write",
-                                    "amxfp4_paged_read", "amxfp4_paged_attention"};
+                                    "amxfp4_paged_read", "amxfp4_paged_attention", "amxfp4_paged_attention_scored", "amxfp4_attention_masked",
+                                    "amxfp4_token_logprobs"};
 constexpr size_t kNumEntries = sizeof(kEntries) / sizeof(kEntries[0]);
 static_assert(sizeof(entry) == kNumEntries * sizeof(void*), "one name per entry point");
 
@@ -345,19 +350,31 @@ PyObject* paged_read(PyObject*, PyObject* const* args, Py_ssize_t n) try {
   Py_RETURN_NONE;
 }
 
-// paged_attention(fmt, q, pool, table, lens, starts, positions, scale, max_keys, out, workspace)
+// cap (float) and slopes (float32 [heads] or None): whether they can be taken
+bool scores(PyObject* cap, PyObject* slopes, int64_t heads, amx_scores_t& s) {
+  if (!PyFloat_CheckExact(cap)) return false;
+  s = {(float)PyFloat_AS_DOUBLE(cap), 0, nullptr};
+  if (slopes == Py_None) return true;
+  const at::Tensor* t = here(slopes);
+  if (!t || t->scalar_type() != at::kFloat || t->dim() != 1 || t->numel() != heads) return false;
+  s.slopes = static_cast<const float*>(t->data_ptr());
+  return true;
+}
+
+// paged_attention(fmt, q, pool, table, lens, starts, positions, scale, max_keys, out, workspace[, cap, slopes])
 PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n) try {
   amx_format_t f;
   amx_paged_pool_t p;
+  amx_scores_t sc;
   const at::Tensor *q, *out, *ws;
   int64_t seqs, max_pages, max_keys;
-  if (n != 11 || !format(args[0], f) || !(q = here(args[1])) || !pool(args[2], f, p) || !PyFloat_CheckExact(args[7]) || !integer(args[8], max_keys) ||
-      !(out = here(args[9])) || !(ws = here(args[10])))
+  if ((n != 11 && n != 13) || !format(args[0], f) || !(q = here(args[1])) || !pool(args[2], f, p) || !PyFloat_CheckExact(args[7]) ||
+      !integer(args[8], max_keys) || !(out = here(args[9])) || !(ws = here(args[10])))
     Py_RETURN_NONE;
   int32_t *lens = ints(args[4], -1, &seqs), *table, *starts, *positions;
   if (!lens || q->scalar_type() != at::kBFloat16 || q->dim() != 3 || q->size(2) != p.head_dim || out->scalar_type() != at::kBFloat16 ||
       out->numel() != q->numel() || !(table = block_table(args[3], seqs, max_pages)) || !(starts = ints(args[5], seqs + 1)) ||
-      !(positions = ints(args[6], q->size(0))))
+      !(positions = ints(args[6], q->size(0))) || (n == 13 && !scores(args[11], args[12], q->size(1), sc)))
     Py_RETURN_NONE;
   const int64_t rows = q->size(0), heads = q->size(1);
   const float scale = (float)PyFloat_AS_DOUBLE(args[7]);
@@ -365,7 +382,77 @@ PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n) try {
   void *to = out->data_ptr(), *scratch = ws->data_ptr();
   const size_t ws_bytes = size_of(ws);
   return run([&](void* s) {
-    return entry.paged_attention(&f, &p, from, rows, heads, table, seqs, max_pages, lens, starts, positions, scale, max_keys, to, scratch, ws_bytes, s);
+    return n == 13 ? entry.paged_attention_scored(&f, &p, from, rows, heads, table, seqs, max_pages, lens, starts, positions, scale, &sc, max_keys, to,
+                                                  scratch, ws_bytes, s)
+                   : entry.paged_attention(&f, &p, from, rows, heads, table, seqs, max_pages, lens, starts, positions, scale, max_keys, to, scratch, ws_bytes, s);
+  });
+} catch (const std::exception&) {
+  Py_RETURN_NONE;
+}
+
+// attention_masked(fmt, q_codes, q_scales, k_codes, k_scales, v_codes, v_scales, scale, causal, pos0, first or None, last or None, cap, slopes or
+// None, out, workspace)
+PyObject* attention_masked(PyObject*, PyObject* const* args, Py_ssize_t n) try {
+  amx_format_t f;
+  amx_scores_t sc;
+  const at::Tensor *t[6], *out, *ws;
+  int64_t pos0;
+  if (n != 16 || !format(args[0], f)) Py_RETURN_NONE;
+  for (int i = 0; i < 6; ++i)
+    if (!(t[i] = here(args[1 + i])) || t[i]->scalar_type() != at::kByte || t[i]->dim() != (i % 2 && f.asymmetric ? 4 : 3)) Py_RETURN_NONE;
+  if (!heads(t) || !PyFloat_CheckExact(args[7]) || !PyBool_Check(args[8]) || !integer(args[9], pos0) || !(out = here(args[14])) || !(ws = here(args[15])))
+    Py_RETURN_NONE;
+  for (int i = 0; i < 6; i += 2)  // a scale, or a pair, to 16 bytes of codes
+    if (t[i + 1]->size(0) != t[i]->size(0) || t[i + 1]->size(1) != t[i]->size(1) || t[i]->size(2) % 16 || t[i + 1]->size(2) != t[i]->size(2) / 16 ||
+        (f.asymmetric && t[i + 1]->size(3) != 2))
+      Py_RETURN_NONE;
+  const int64_t Hq = t[0]->size(0), Sq = t[0]->size(1), D = t[0]->size(2) * 2, Hkv = t[2]->size(0), Sk = t[2]->size(1);
+  const int32_t *first = nullptr, *last = nullptr;
+  if ((args[10] != Py_None && !(first = ints(args[10], Sq))) || (args[11] != Py_None && !(last = ints(args[11], Sq))) ||
+      !scores(args[12], args[13], Hq, sc) || out->scalar_type() != at::kBFloat16 || out->numel() != Sq * Hq * D)
+    Py_RETURN_NONE;
+  uint8_t* p[6];
+  for (int i = 0; i < 6; ++i) p[i] = bytes(t[i]);
+  const float scale = (float)PyFloat_AS_DOUBLE(args[7]);
+  const bool causal = args[8] == Py_True;
+  void *to = out->data_ptr(), *scratch = ws->data_ptr();
+  const size_t ws_bytes = size_of(ws);
+  return run([&](void* s) {
+    return entry.attention_masked(&f, Hq, Hkv, Sq, Sk, D, p[0], p[1], p[2], p[3], p[4], p[5], scale, &sc, causal, pos0, first, last, to, scratch,
+                                  ws_bytes, s);
+  });
+} catch (const std::exception&) {
+  Py_RETURN_NONE;
+}
+
+// token_logprobs(logits, targets or None, top, cap, (logprobs, entropy, top_logprobs, top_ids), workspace)
+PyObject* token_logprobs(PyObject*, PyObject* const* args, Py_ssize_t n) try {
+  const at::Tensor *x, *ws;
+  int64_t top;
+  if (n != 6 || !(x = tensor(args[0])) || !integer(args[2], top) || !PyFloat_CheckExact(args[3]) || !PyTuple_Check(args[4]) ||
+      PyTuple_GET_SIZE(args[4]) != 4 || !(ws = here(args[5])))
+    Py_RETURN_NONE;
+  const bool bf16 = x->scalar_type() == at::kBFloat16;
+  if ((!bf16 && x->scalar_type() != at::kFloat) || x->dim() != 2 || x->stride(1) != 1 || x->get_device() != c10::hip::current_device()) Py_RETURN_NONE;
+  const int64_t rows = x->size(0), vocab = x->size(1), ld = rows > 1 ? x->stride(0) : vocab;
+  const int32_t* targets = nullptr;
+  if (args[1] != Py_None && !(targets = ints(args[1], rows))) Py_RETURN_NONE;
+  void* out[4] = {};
+  for (int i = 0; i < 4; ++i) {
+    PyObject* o = PyTuple_GET_ITEM(args[4], i);
+    if (o == Py_None) continue;
+    const at::Tensor* t = here(o);
+    if (!t || t->scalar_type() != (i == 3 ? at::kInt : at::kFloat) || t->dim() != (i < 2 ? 1 : 2) || t->size(0) != rows || (i >= 2 && t->size(1) != top))
+      Py_RETURN_NONE;
+    out[i] = t->numel() ? t->data_ptr() : nullptr;
+  }
+  const float cap = (float)PyFloat_AS_DOUBLE(args[3]);
+  const void* from = x->data_ptr();
+  void* scratch = ws->data_ptr();
+  const size_t ws_bytes = size_of(ws);
+  return run([&](void* s) {
+    return entry.token_logprobs(from, bf16 ? 1 : 0, rows, vocab, ld, targets, cap, top, static_cast<float*>(out[0]), static_cast<float*>(out[1]),
+                                static_cast<float*>(out[2]), static_cast<int32_t*>(out[3]), scratch, ws_bytes, s);
   });
 } catch (const std::exception&) {
   Py_RETURN_NONE;
@@ -391,7 +478,7 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define CALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {CALL(quantize), CALL(quantize_batched), CALL(tensor_scale), CALL(gemm), CALL(gemm_prepared),
                           CALL(attention), CALL(attention_decode), CALL(paged_plan), CALL(paged_write), CALL(paged_read),
-                          CALL(paged_attention), CALL(bind), {nullptr, nullptr, 0, nullptr}};
+                          CALL(paged_attention), CALL(attention_masked), CALL(token_logprobs), CALL(bind), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -10,7 +10,7 @@
 // A capped logit is x (1 + u P(u)), u = (x / cap)^2, up to 0.6 of the cap, which is most segments; in the others each value takes what
 // is its due. Logits of -inf have a path of their own too: there the differences are kept from 0 times infinity.
 //
-// Alternatives. A row is read in segments (4 chunks of 16 bytes to a lane, side by side over the wave); each leaves its largest logit
+// Alternatives. A row is read in segments (chunks of 16 bytes to a lane, side by side over the wave); each leaves its largest logit
 // in LDS, each thread keeps its own. The top-th largest of a wave's 64 and of the segments' bound the result from below, so only
 // segments that reach the bound are read again, from the cache, and the few elements at or above it are put in order by counting for
 // each how many are better. Rows in which more than kList elements reach the bound (equal logits by the hundred, fewer tokens than `top`
@@ -24,7 +24,7 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kChunks = 4;      // of 16 bytes, to a lane and segment
+constexpr int kSegment = 1024;  // elements, 16 to a lane
 constexpr int kSegments = 512;  // of a part, at most
 constexpr int kList = 512;      // candidates that are put in order at once
 constexpr int kMostTop = 64;
@@ -73,8 +73,6 @@ __device__ __forceinline__ Sums wave_joined(Sums a) {
   return {m, wave_sum(a.s), wave_sum(a.t)};
 }
 
-__device__ __forceinline__ bool is_better(float v, int i, float w, int j) { return v > w || (v == w && i < j); }
-
 struct LogprobWork {
   const void* logits;
   const int32_t* targets;
@@ -99,61 +97,78 @@ __device__ __forceinline__ float value_of(const LogprobWork& w, float x) {
   return x == -INFINITY ? x : __builtin_fabsf(x) <= w.small ? capped_small(w, x) : capped(x, w.in, w.cap);
 }
 
+// A logit and its id as one number, larger for what is better (no NaN; zeros of both signs are equal).
+__device__ __forceinline__ uint64_t key_of(float v, int id) {
+  const uint32_t u = f2u(v + 0.f), up = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+  return (uint64_t)up << 32 | (uint32_t)~id;
+}
+__device__ __forceinline__ float logit_of(uint64_t key) {
+  const uint32_t up = (uint32_t)(key >> 32);
+  return u2f(up ^ ((uint32_t)((int32_t)~up >> 31) | 0x80000000u));
+}
+__device__ __forceinline__ int id_of(uint64_t key) { return (int)~(uint32_t)key; }
+
 struct Selection {
-  float list_v[kList];
-  int list_i[kList];
-  float wave_v[kWaves];
-  int wave_i[kWaves];
+  uint64_t list[kList];
+  uint64_t wave_best[kWaves];
   int count;
 };
 
-// The k best of the elements that each(f) hands to this thread as f(logit, id), k in all threads together, in order: emit(rank, logit, id).
-// No element below `bound` is among them. What is not there (of rows with NaN) comes out as id -1. l.count is 0.
-template <class Each, class Emit>
+// The k best of the elements that each(f) hands to this thread as f(logit, id, there), k in all threads together, in order: emit(rank, logit,
+// id). f comes for N elements at a time, `there` false for those that are none. No element below `bound` is among them. What is not there (of
+// rows with NaN) comes out as id -1. l.count is 0.
+template <int N, class Each, class Emit>
 __device__ __forceinline__ void select_best(Selection& l, int k, float bound, Each each, Emit emit) {
   const int t = threadIdx.x;
-  each([&](float v, int i) {
-    if (v >= bound) {
-      const int at = atomicAdd(&l.count, 1);
-      if (at < kList) l.list_v[at] = v, l.list_i[at] = i;
-    }
+  each([&](const float (&v)[N], auto id, auto there) {
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) mine += v[i] >= bound && there(i) ? 1 : 0;
+    if (mine == 0) return;
+    int at = atomicAdd(&l.count, mine);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (v[i] >= bound && there(i)) {
+        if (at < kList) l.list[at] = key_of(v[i], id(i));
+        ++at;
+      }
   });
   __syncthreads();
   const int n = l.count;
   if (n <= kList) {
     for (int c = t; c < n; c += kThreads) {
-      const float v = l.list_v[c];
-      const int i = l.list_i[c];
+      const uint64_t key = l.list[c];
       int rank = 0;
 #pragma unroll 8
-      for (int o = 0; o < n; ++o) rank += is_better(l.list_v[o], l.list_i[o], v, i) ? 1 : 0;
-      if (rank < k) emit(rank, v, i);
+      for (int o = 0; o < n; ++o) rank += l.list[o] > key ? 1 : 0;
+      if (rank < k) emit(rank, logit_of(key), id_of(key));
     }
     for (int r = n + t; r < k; r += kThreads) emit(r, NAN, -1);
     return;
   }
-  float last_v = INFINITY;
-  int last_i = -1;
+  uint64_t last = ~uint64_t(0);
   for (int r = 0; r < k; ++r) {
-    float v = -INFINITY;
-    int i = 0x7FFFFFFF;
-    each([&](float x, int j) {
-      if (is_better(last_v, last_i, x, j) && is_better(x, j, v, i)) v = x, i = j;
+    uint64_t best = 0;  // (less than any element's)
+    each([&](const float (&v)[N], auto id, auto there) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (v[i] >= bound && there(i)) {
+          const uint64_t key = key_of(v[i], id(i));
+          if (key < last && key > best) best = key;
+        }
     });
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
-      const float ov = __shfl_xor(v, o, 64);
-      const int oi = __shfl_xor(i, o, 64);
-      if (is_better(ov, oi, v, i)) v = ov, i = oi;
+      const uint64_t other = __shfl_xor(best, o, 64);
+      best = other > best ? other : best;
     }
     __syncthreads();  // (the last round's have been read)
-    if ((t & 63) == 0) l.wave_v[t >> 6] = v, l.wave_i[t >> 6] = i;
+    if ((t & 63) == 0) l.wave_best[t >> 6] = best;
     __syncthreads();
 #pragma unroll
-    for (int o = 0; o < kWaves; ++o)
-      if (is_better(l.wave_v[o], l.wave_i[o], v, i)) v = l.wave_v[o], i = l.wave_i[o];
-    if (t == 0) emit(r, i == 0x7FFFFFFF ? NAN : v, i == 0x7FFFFFFF ? -1 : i);
-    last_v = v, last_i = i;
+    for (int o = 0; o < kWaves; ++o) best = l.wave_best[o] > best ? l.wave_best[o] : best;
+    if (t == 0) emit(r, best ? logit_of(best) : NAN, best ? id_of(best) : -1);
+    last = best;
   }
 }
 
@@ -183,8 +198,7 @@ __device__ __forceinline__ float logprob_of(const LogprobWork& w, Sums all, floa
 template <bool BF16, bool CAP, bool TOP>
 __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(LogprobWork w) {
   using Element = std::conditional_t<BF16, uint16_t, float>;
-  constexpr int kE = 16 / (int)sizeof(Element), kN = kChunks * kE;  // elements of a chunk; of a lane and segment
-  constexpr int kSegment = 64 * kN;
+  constexpr int kE = 16 / (int)sizeof(Element), kN = kSegment / 64, kChunks = kN / kE;  // elements of a chunk of 16 bytes; of a lane; its chunks
   __shared__ Selection l;
   __shared__ Sums wave_sums[kWaves];
   __shared__ float segment_best[TOP ? kSegments : 1];
@@ -237,7 +251,10 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(LogprobWork w)
           }
         } else {
 #pragma unroll
-          for (int e = 0; e < kE; ++e) v[c * kE + e] = i + e >= 0 && i + e < w.vocab ? value(x[i + e]) : -INFINITY;
+          for (int e = 0; e < kE; ++e) {  // (all asked for before the first is looked at)
+            const float at = value(x[min(max(i + e, 0), w.vocab - 1)]);
+            v[c * kE + e] = i + e >= 0 && i + e < w.vocab ? at : -INFINITY;
+          }
         }
       }
     }
@@ -247,8 +264,8 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(LogprobWork w)
   if (t == 0) l.count = 0, chosen_count = 0;
   Sums mine = {-INFINITY, 0.f, 0.f};
   float best = -INFINITY;  // of the thread, as logits
+  float v[kN];
   for (int s = s0 + wave; s < s1; s += kWaves) {
-    float v[kN];
     load(s, v);
     float most = v[0], edge = CAP ? __builtin_fabsf(v[0]) : v[0];  // edge: the largest size, or the smallest value
 #pragma unroll
@@ -314,21 +331,27 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(LogprobWork w)
       __syncthreads();
       bound = fmaxf(bound, fminf(fminf(bounds[1][0], bounds[1][1]), fminf(bounds[1][2], bounds[1][3])));
     }
-    for (int s = t; s < segments; s += kThreads)
-      if (segment_best[s] >= bound) chosen[atomicAdd(&chosen_count, 1)] = s;
-    __syncthreads();
-    const int count = chosen_count;
+    int count = 0;
+    if (segments > kWaves) {  // (uniform)
+      for (int s = t; s < segments; s += kThreads)
+        if (segment_best[s] >= bound) chosen[atomicAdd(&chosen_count, 1)] = s;
+      __syncthreads();
+      count = chosen_count;
+    }
     auto each = [&](auto f) {
+      auto segment = [&](int s) {
+        const int first = s * kSegment - off + lane * kE;
+        auto id = [&](int i) { return first + i / kE * 64 * kE + i % kE; };
+        f(v, id, [&](int i) { return id(i) >= 0 && id(i) < w.vocab; });
+      };
+      if (segments <= kWaves) {  // a wave has read one at most, and has it still
+        if (wave < segments) segment(s0 + wave);
+        return;
+      }
       for (int c = wave; c < count; c += kWaves) {
         const int s = s0 + chosen[c];
-        float v[kN];
         load(s, v);
-        const int first = s * kSegment - off + lane * kE;
-#pragma unroll
-        for (int i = 0; i < kN; ++i) {
-          const int id = first + i / kE * 64 * kE + i % kE;
-          if (id >= 0 && id < w.vocab) f(v[i], id);
-        }
+        segment(s);
       }
     };
     auto emit = [&](int rank, float v, int id) {
@@ -337,7 +360,7 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(LogprobWork w)
       else
         w.tops[(int64_t)blockIdx.x * k + rank] = make_uint2(f2u(v), (uint32_t)id);
     };
-    select_best(l, k, bound, each, emit);
+    select_best<kN>(l, k, bound, each, emit);
   }
 }
 
@@ -380,35 +403,43 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_join_kernel(LogprobWo
     __syncthreads();
     auto each = [&](auto f) {
       for (int i = t; i < parts * k; i += kThreads) {
-        const uint2 v = tops[i];
-        if ((int)v.y >= 0) f(u2f(v.x), (int)v.y);
+        const uint2 entry = tops[i];
+        const float v[1] = {u2f(entry.x)};
+        f(v, [&](int) { return (int)entry.y; }, [&](int) { return (int)entry.y >= 0; });
       }
     };
     auto emit = [&](int rank, float v, int id) {
       w.top_logprobs[row * k + rank] = logprob_of<CAP>(w, all, log_s, v), w.top_ids[row * k + rank] = id;
     };
-    select_best(l, k, bound, each, emit);
+    select_best<1>(l, k, bound, each, emit);
   }
 }
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-int segment_of(int dtype) { return 64 * kChunks * 16 / (dtype == 1 ? 2 : 4); }
-
-// Parts that a row is read in, and segments of each. Rows enough to fill the chip are read whole.
+// Parts that a row is read in, and segments of each: as many as give 1024 workgroups, and more for long rows, up to 3000, as long as a part has
+// 128 KB. Rows of 1024 and more are read whole. us with up to 1024, 2048 and 4096 workgroups: 300 rows of 32000 BF16 logits 16.5, 21.5 and
+// 19.1, 2000 of 128000 BF16 120, 132 and 146, 700 of 256000 float32 154, 140 and 135, 4000 of 32001 float32 108, 108 and 122.
 int parts_of(int dtype, int64_t rows, int64_t vocab, int& per_part) {
-  const int64_t segments = (vocab + 7 + segment_of(dtype) - 1) / segment_of(dtype);  // (a row may begin up to 7 elements behind a boundary)
-  int64_t parts = (2048 + rows - 1) / rows;
+  const int64_t segments = (vocab + 7 + kSegment - 1) / kSegment;  // (a row may begin up to 7 elements behind a boundary)
+  const int64_t large = vocab * (dtype == 1 ? 2 : 4) >> 17, many = 3000 / rows;
+  int64_t parts = (1024 + rows - 1) / rows;
+  const int64_t more = many < large ? many : large;
+  parts = parts > more ? parts : more;
   const int64_t most = (segments + kWaves - 1) / kWaves, least = (segments + kSegments - 1) / kSegments;
   parts = parts < most ? parts : most;
   parts = parts < kMostParts ? parts : kMostParts;
   parts = parts > least ? parts : least;
   per_part = (int)((segments + parts - 1) / parts);
+  // (a segment to each wave, or as many: with one more the others wait, and up to one each they need not be read again. 96 rows of 50001 BF16
+  // logits in parts of four 13.7 us, of five 15.3)
+  const int even = per_part / kWaves * kWaves;
+  if (even > 0 && (segments + even - 1) / even <= kMostParts) per_part = even;
   return (int)((segments + per_part - 1) / per_part);
 }
 
 constexpr int64_t kMostVocab = int64_t(1) << 24, kMostRows = int64_t(1) << 23;
-static_assert(kMostVocab / 1024 / kSegments < kMostParts, "a part's segments fit");
+static_assert(kMostVocab / kSegment / kSegments < kMostParts, "a part's segments fit");
 
 bool bad_shape(int32_t dtype, int64_t rows, int64_t vocab, int64_t top) {
   return (dtype != 0 && dtype != 1) || rows <= 0 || rows > kMostRows || vocab <= 0 || vocab > kMostVocab || top < 0 || top > kMostTop || top > vocab;

@@ -15,6 +15,9 @@ MLP width F:
 With fused_attention=True the two attention products and the softmax between them are one call (binding.attention):
 the attention map is not materialised and its tiles are cast relative to the running row maximum, which gives
 slightly different numbers than casting the normalised map.
+With score_cap, slopes or a range of keys for each row (packed documents, prefixes, windows) it is binding.attention_masked, and step() hands
+cap and slopes on too. LMHead is what follows the last layer when text is scored: the normalisation, the product with the vocabulary's
+weights and the log probabilities, a number of rows at a time.
 step() is the same layer for sequences that are being served: their new rows, packed into one batch, against the keys and values
 that a PagedCache holds. The queries and the probabilities stay BF16 there; keys and values are cast per token along D.
 """
@@ -35,6 +38,7 @@ class LayerConfig:
     d_ff: int = 14336
     eps: float = 1e-5
     rope_theta: float = 500000.0
+    score_cap: float = 0.0  # attention scores s become score_cap tanh(s / score_cap); 0: as they are
 
 
 WEIGHT_SHAPES = lambda c: {  # noqa: E731  (name -> [out features, in features])
@@ -77,8 +81,11 @@ class DecoderLayer:
     cast once here (they are static in inference); forward() casts the activations."""
 
     def __init__(self, cfg, weights, fmt, baseline=False, fused_attention=False, fused_glu=None, fused_norm=None,
-                 fused_rope=None, prepared_weights=False):
+                 fused_rope=None, prepared_weights=False, slopes=None):
+        """slopes: float32 [n_heads] on the GPU: scores of a head fall by so much for each key of distance (with or without a cap, these need
+        fused_attention in forward())."""
         self.cfg, self.fmt, self.baseline, self.fused_attention = cfg, fmt, baseline, fused_attention
+        self.slopes = slopes
         # the rotary embedding casts its result (Q and K never exist as BF16 tensors): same bits
         if fused_rope is None:
             fused_rope = fmt.group_size == 32 and cfg.head_dim % 64 == 0 and cfg.head_dim <= 256
@@ -131,8 +138,14 @@ class DecoderLayer:
     def _cast(self, x, k_axis=-1):
         return binding.quantize(self.fmt, x, k_axis=k_axis, baseline=self.baseline)
 
-    def forward(self, x, pos0=0):
+    def forward(self, x, pos0=0, first=None, last=None):
+        """x BF16 [rows, d_model], rows a multiple of 32, the first at position pos0. first, last: int32 [rows] on the GPU: the first and the last of
+        these rows that each of them sees, as binding.attention_masked() takes them (last instead of the causal mask: none behind the row
+        itself is kept from it then); they need fused_attention."""
         c = self.cfg
+        masked = first is not None or last is not None or c.score_cap or self.slopes is not None
+        if masked and not self.fused_attention:
+            raise binding.AmxError("forward: ranges of keys, score_cap and slopes need fused_attention")
         S, G, D = x.shape[0], c.n_kv_heads, c.head_dim
         per = c.n_heads // G
         nsc = self.wqkv[1].shape[2:]  # () or (2,): scale entries per group
@@ -151,6 +164,13 @@ class DecoderLayer:
         if self.fused_attention:
             vc, vs = self._cast_v(v, nsc)
             fmt = binding.make_format(self.fmt.scale, False, 32) if self.baseline else self.fmt
+            if masked:
+                need = binding.attention_masked_workspace_bytes(fmt, c.n_heads, G, S, S, D)
+                o = binding.attention_masked(fmt, qc.view(c.n_heads, S, D // 2), qs.view(c.n_heads, S, D // 32, *nsc), kc.view(G, S, D // 2),
+                                             ks.view(G, S, D // 32, *nsc), vc, vs, 1.0 / math.sqrt(D), causal=last is None, first=first, last=last,
+                                             cap=c.score_cap, slopes=self.slopes, workspace=self._workspace(need, x.device),
+                                             out=torch.empty((S, c.n_heads * D), dtype=torch.bfloat16, device=x.device))
+                return self._after_attention(x, o)
             need = binding.attention_workspace_bytes(fmt, c.n_heads, G, S, S, D)
             # (the kernel writes its output merged and in BF16: what merge_heads would make of the FP32 result)
             o = binding.attention(fmt, qc.view(c.n_heads, S, D // 2), qs.view(c.n_heads, S, D // 32, *nsc),
@@ -188,7 +208,7 @@ class DecoderLayer:
         need = binding.paged_attention_workspace_bytes(fmt, pool, rows, c.n_heads, cache.lens.numel(), max_keys)
         attn = torch.empty((rows, c.n_heads * c.head_dim), dtype=torch.bfloat16, device=x.device)
         binding.paged_attention(fmt, q, pool, cache.table, plan.lens, plan.starts, plan.positions, 1.0 / math.sqrt(c.head_dim), max_keys,
-                                out=attn, workspace=self._workspace(need, x.device))
+                                out=attn, workspace=self._workspace(need, x.device), cap=c.score_cap, slopes=self.slopes)
         return self._after_attention(x, attn)
 
     def _cast_v(self, v, nsc):
@@ -230,3 +250,29 @@ class DecoderLayer:
         pairs = S * (S + 32) // 2 if (self.fused_attention and not nominal) else S * S
         att = 2 * c.n_heads * pairs * c.head_dim
         return 2.0 * (lin + att)
+
+
+class LMHead:
+    """What turns the last layer's output into log probabilities of tokens. weight: BF16 CUDA tensor [vocab, d_model], cast once here; norm: FP32
+    [d_model], the normalisation in front of it; cap: logits x become cap tanh(x / cap). The logits exist for `rows_at_once` rows at a time."""
+
+    def __init__(self, weight, norm, fmt, eps=1e-5, cap=0.0, rows_at_once=1024):
+        self.fmt, self.eps, self.cap, self.rows_at_once = fmt, eps, cap, rows_at_once
+        self.weight = binding.quantize(fmt, weight.contiguous())
+        self.norm = norm.contiguous()
+
+    def logits(self, x):
+        """FP32 [rows, vocab] of x BF16 [rows, d_model], before the cap."""
+        return binding.gemm(self.fmt, *binding.rmsnorm_quantize(self.fmt, x, self.norm, self.eps), *self.weight)
+
+    def logprobs(self, x, targets=None, top=0):
+        """binding.token_logprobs() of the rows x BF16 [rows, d_model]."""
+        rows = x.shape[0]
+        f = lambda *shape: torch.empty(shape, dtype=torch.float32, device=x.device)  # noqa: E731
+        out = binding.TokenLogprobs(None if targets is None else f(rows), f(rows), f(rows, top) if top else None,
+                                    torch.empty((rows, top), dtype=torch.int32, device=x.device) if top else None)
+        for at in range(0, rows, self.rows_at_once):
+            part = slice(at, at + self.rows_at_once)
+            binding.token_logprobs(self.logits(x[part]), None if targets is None else targets[part], top, self.cap,
+                                   out=tuple(None if t is None else t[part] for t in out))
+        return out

@@ -10,6 +10,7 @@ from oracle import ref, scoring_ref
 from paper_2411_09909_amd import binding
 from tests import gpu_util as G
 from tests.test_gpu_attention_fused import heads
+from tests.test_gpu_calls import taken
 
 pytestmark = pytest.mark.gpu
 FORMATS = [(ref.FP8_E5M2, 1), (ref.FP8_E5M2, 0), (ref.FP8_E4M3, 1), (ref.E8M0_FLOOR, 1), (ref.E8M0_FLOOR, 0), (ref.E8M0_ROUND, 1)]
@@ -180,6 +181,23 @@ def test_another_stream_a_graph_and_calls_at_the_same_time(Sq, Sk):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, call())
+
+
+def test_the_native_way(monkeypatch):
+    """With all buffers given the call goes through the native module: the same bits."""
+    fmt, ops = operands(heads(4, 70, 1), heads(2, 96, 2), heads(2, 96, 3), ref.FP8_E5M2, 1)
+    first, slopes = ints(np.arange(70) - 20), torch.from_numpy(slopes_of(4)).cuda()
+    for how in (dict(), dict(first=first, pos0=20), dict(last=first, causal=False, cap=30), dict(first=first, last=first + 9, slopes=slopes, cap=0.0)):
+        want = binding.attention_masked(fmt, *ops, 0.1, **how)
+        spy = taken(monkeypatch, "attention_masked")
+        out = torch.zeros_like(want)
+        got = binding.attention_masked(fmt, *ops, 0.1, **how, out=out, workspace=torch.empty(1 << 20, dtype=torch.uint8, device="cuda"))
+        assert spy.count == 1 and got is out and torch.equal(want, got)
+        monkeypatch.undo()
+    out, ws = torch.zeros(70, 512, dtype=torch.bfloat16, device="cuda"), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    for bad in (dict(first=first[:69]), dict(slopes=slopes[:3]), dict(slopes=slopes.double()), dict(out=out[:69]), dict(workspace=ws[:256]), dict(cap=-1.0)):
+        with pytest.raises(binding.AmxError):
+            binding.attention_masked(fmt, *ops, 0.1, **{**dict(out=out, workspace=ws), **bad})
 
 
 def test_wrong_tensors_are_refused():

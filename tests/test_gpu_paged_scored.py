@@ -9,6 +9,7 @@ import torch
 from oracle import scoring_ref
 from paper_2411_09909_amd import binding
 from tests.test_gpu_attention_masked import slopes_of
+from tests.test_gpu_calls import taken
 from tests.test_gpu_paged import FORMATS, allowed, bits, dev, f64, filled, host_pool
 
 pytestmark = pytest.mark.gpu
@@ -92,7 +93,7 @@ def test_slopes_of_zero_and_a_wide_cap_change_little():
         assert (a - b).norm() <= 2.0 ** -7 * a.norm()
 
 
-def test_a_graph():
+def test_the_native_way_and_a_graph(monkeypatch):
     rng = np.random.RandomState(10)
     fmt, pool, table = filled(rng, "amxfp4_e5m2", 2, 128, 64, [3000, 1200], 48)
     q = torch.randn(2, 8, 128, device="cuda").to(torch.bfloat16)
@@ -101,6 +102,13 @@ def test_a_graph():
     out = torch.zeros(2, 1024, dtype=torch.bfloat16, device="cuda")
     ws = torch.empty(binding.paged_attention_workspace_bytes(fmt, pool, 2, 8, 2, 0), dtype=torch.uint8, device="cuda")
     binding.paged_attention(*args, cap=30.0, slopes=slopes)
+    spy = taken(monkeypatch, "paged_attention")  # with all buffers given: through the native module
+    want = binding.paged_attention(*args, cap=30.0, slopes=slopes)
+    assert binding.paged_attention(*args, cap=30, slopes=slopes, out=out, workspace=ws) is out and spy.count == 1 and torch.equal(out, want)
+    for bad in (dict(cap=-1.0), dict(slopes=slopes[:7]), dict(slopes=slopes.cpu())):
+        with pytest.raises(binding.AmxError):
+            binding.paged_attention(*args, **{**dict(slopes=slopes), **bad}, out=out, workspace=ws)
+    monkeypatch.undo()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         binding.paged_attention(*args, cap=30.0, slopes=slopes, out=out, workspace=ws)

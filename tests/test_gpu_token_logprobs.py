@@ -5,6 +5,7 @@ import torch
 
 from oracle import scoring_ref
 from paper_2411_09909_amd import binding
+from tests.test_gpu_calls import taken
 
 pytestmark = pytest.mark.gpu
 INF = float("inf")
@@ -179,6 +180,25 @@ def test_another_stream_and_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(binding.token_logprobs(x, t, 10), out))
+
+
+def test_the_native_way(monkeypatch):
+    """With all buffers given the calls go through the native module; what it does not take is refused as before."""
+    x, t = torch.randn(3, 700, device="cuda"), torch.tensor([1, 2, 700], dtype=torch.int32, device="cuda")
+    want = binding.token_logprobs(x, t, 4, 30.0)
+    for targets, top, drop in ((t, 4, ()), (None, 4, (0,)), (t, 0, (2, 3)), (t, 4, (1,))):
+        spy = taken(monkeypatch, "token_logprobs")
+        out = tuple(None if i in drop else torch.zeros_like(a) for i, a in enumerate(want))
+        got = binding.token_logprobs(x, targets, top, 30, out=out, workspace=torch.empty(1 << 20, dtype=torch.uint8, device="cuda"))
+        assert spy.count == 1 and all(b is None or torch.equal(a, b) for a, b in zip(want, got))
+        monkeypatch.undo()
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    good = [torch.zeros_like(a) for a in want]
+    for i, bad in ((0, good[0][:2]), (1, good[1].double()), (2, good[2][:, :3]), (3, good[3].float()), (2, good[2].cpu())):
+        with pytest.raises(binding.AmxError):
+            binding.token_logprobs(x, t, 4, out=[bad if j == i else a for j, a in enumerate(good)], workspace=ws)
+    with pytest.raises(binding.AmxError):
+        binding.token_logprobs(torch.randn(1, 200000, device="cuda"), out=(None, good[1][:1], None, None), workspace=ws[:256])  # too small
 
 
 def test_wrong_tensors_are_refused():
