@@ -9,7 +9,21 @@
 //
 // Ranges. A lane keeps its query's first key and the number of keys behind it; the mask of a score is one subtraction and one
 // unsigned comparison. The wave's smallest first and largest last key bound the tiles it computes, the workgroup's those it loads; tiles that
-// all of a wave's queries see wholly skip the mask. A query that has seen no key yet keeps its sums as they are.
+// all of a wave's queries see wholly skip the mask. The running maximum begins at the lowest finite number, so that a query that has seen no
+// key yet has weights of 0 and a factor of 1 without a test.
+// Scores. In units of log2. Where they rise with the products (no slopes) the maximum is taken of those, and a score less the maximum and the
+// scale's logarithm is one multiply-add (capped: the last step of a polynomial). A slope is a constant of the key's place in the tile, added by
+// that step too, and one number for the tile, which only the maximum sees.
+// Split rows (kMaxima, kPart). The cast of a tile depends on the running maximum of all keys before it, so chunks of the keys are not
+// independent; but the maximum is a fifth of the work (half of the products and no exponentials). One launch takes every chunk's
+// maxima, the next starts each chunk with those of the chunks before it, and the join adds the sums up: the same numbers as without the split.
+//
+// Bound and measured (us a call with the expansion of K and V in front; cards differ by 4 %): 32 / 8 heads of 128 x 8192 with slopes 580 = 948 TFLOP/s of
+// the visible half, with nothing but the causal mask 536 (amxfp4_attention: 567), the rate of a library's product of 8192^3 being 1200 to 1420. A
+// tile of a wave is 16 products of 32 cycles and some 600 cycles of vector instructions, 1200 together: the two pipes hardly overlap. 2048 rows of nine
+// documents with capped scores 42, of which the expansion is 8: blocks of very different length, all running at once. The first form took 834 and 55: the
+// accumulator in the second half of the register file, copied back and forth (waves_per_eu given no lower bound), the mask computed for every
+// tile, exp2 and a reciprocal for each capped score, two exchanges through LDS to a tile.
 #include "attention_tile.h"
 #include "cast_math.h"
 #include "dequant_regs.h"
@@ -34,7 +48,7 @@ struct MaskedWork {
   int Sq, Sk, kv_group, causal, pos0;
   float *maxima, *parts;  // of split rows: [head][row][chunk]; [head][chunk][row][D]
   float2* ends;           // [head][chunk][row]: maximum and sum
-  int turn;  // query blocks to a turn of the workgroups over the compute units (0: blocks in descending order)
+  int turn;  // query blocks to a turn of the workgroups over the compute units (0: the last block first)
   Scores scores;
 };
 
@@ -57,6 +71,9 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
     const uint16_t* __restrict__ Vp, uint16_t* __restrict__ out, MaskedWork w) {
   // FP8-E5M2 scales: probabilities as FP16 times 2^8, V^T biased by 2^-3, the 2^5 taken out with the row sum at the end
   constexpr bool kPF16 = SCALE_KIND == kScaleE5M2;
+  // Whether a wave goes before the others of its SIMD while it multiplies: 32 / 8 heads of 128 x 4096, causal, 160 -> 154 us, 64 / 8 x 1504 39.7 -> 38.7,
+  // a window of 4096 over 1000 rows of heads of 64, split, 110 -> 106; pairs of tiles, 2048 rows, 74.6 -> 76.2, heads of 64 tile by tile 435 -> 444.
+  constexpr bool kProductsFirst = PASS == kPart || (PASS == kWhole && NT == 1 && D == 128);
   constexpr int kFrags = D / 16, kTileBytes = kFrags * kFragBytes;  // of K, and of V, in a key tile
   // two stages of (K tiles, V tiles), separate arrays so that loads into one stage are known not to alias reads of the other
   __shared__ __attribute__((aligned(1024))) uint8_t ldsK0[NT * kTileBytes];
@@ -67,14 +84,14 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // x walks the query heads, a contiguous range of them per XCD where their number is a multiple of 8; y the query blocks,
-  // the last ones, which have the most key tiles under a causal mask, first
+  // x walks the query heads, a contiguous range of them per XCD where their number is a multiple of 8; y the query blocks: without ranges the
+  // last ones, which have the most key tiles under a causal mask, first
   const int nheads = (int)gridDim.x;
   const int h = (nheads & 7) == 0 ? (int)(blockIdx.x & 7) * (nheads >> 3) + (int)(blockIdx.x >> 3) : (int)blockIdx.x;
   const int g = h / w.kv_group;
   const int blocks = (int)gridDim.y;
   int block = blocks - 1 - (int)blockIdx.y;
-  if (w.turn > 0) {  // uniform
+  if (w.turn > 0) {  // uniform: the blocks by the keys between their first row's first and their last row's last, longest first
     const int b = min(lane, blocks - 1), row0 = b * kQueries, row1 = min(row0 + kQueries, w.Sq) - 1;
     int a = 0, z = w.Sk - 1;
     if (w.first) a = max(w.first[row0], 0);
@@ -225,6 +242,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[n][v] = 0.f;
+    if constexpr (kProductsFirst) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int kb = 0; kb < kFrags; ++kb)
 #pragma unroll
@@ -232,6 +250,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
         const bf16x8 a = *reinterpret_cast<const bf16x8*>(K + n * kTileBytes + kb * kFragBytes + lane_off);
         s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[kb], s[n], 0, 0, 0);
       }
+    if constexpr (kProductsFirst) __builtin_amdgcn_s_setprio(0);
     const bool all_seen = t * 32 >= all_from && (t + NT) * 32 - 1 <= all_to;  // every key of the tiles, by every query (uniform)
     bool small = false;
     if constexpr (CAP) {
@@ -348,6 +367,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
       }
     }
     // ---- O^T
+    if constexpr (kProductsFirst) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       if (__builtin_amdgcn_ballot_w64(alpha[n] != 1.0f) != 0) {  // the maximum moved for some query: rescale
@@ -369,6 +389,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
         }
       }
     }
+    if constexpr (kProductsFirst) __builtin_amdgcn_s_setprio(0);
   };
 
   AMX_WAIT_VMCNT(0);
@@ -441,14 +462,22 @@ __global__ __launch_bounds__(256) void attention_masked_join_kernel(const float*
   *reinterpret_cast<uint2*>(out + ((int64_t)row * heads + h) * D + d) = make_uint2(pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv));
 }
 
-constexpr int64_t kMostOrdered = 768;
-constexpr int64_t kSplitBelow = 256, kSplitInto = 768, kLeastOfChunk = 8, kMostChunks = 32;
+// Up to so many workgroups all run at once. They are dealt to the compute units in turns, of which every other one goes backwards, so that a
+// unit that got a long block in one gets a short one in the next: nine documents in 2048 rows 47 -> 42 us, five prefixes in 1504 rows (64 heads)
+// 48 -> 40. Of more workgroups the longest start first.
+constexpr int64_t kAtOnce = 768;
+constexpr int64_t kMostBlocks = 64;  // (a lane to each)
+
+// Few workgroups with long rows are split over the keys, into about kSplitInto workgroups (twice as many where one wave of four has rows at
+// all), with kLeastOfChunk key tiles or more to each: 10 rows behind 3000 keys, 32 / 8 heads of 128, 92 -> 33 us (with four tiles 37), behind 30000 786 ->
+// 118 (132 with half as many), 100 rows of heads of 64 behind 8000 185 -> 46 (52 with twice as many), 700 rows behind 3000 116 -> 108 (111).
+constexpr int64_t kSplitBelow = 256, kSplitInto = 768, kLeastOfChunk = 8, kMostChunks = 64;
 
 // Chunks that the key tiles of a block of queries are cut into.
 int chunks_of(int64_t Hq, int64_t Sq, int64_t tiles) {
   const int64_t workgroups = Hq * ((Sq + kQueries - 1) / kQueries);
   if (workgroups > kSplitBelow) return 1;
-  int64_t c = (kSplitInto + workgroups - 1) / workgroups;
+  int64_t c = ((Sq <= 32 ? 2 : 1) * kSplitInto + workgroups - 1) / workgroups;
   if (c > tiles / kLeastOfChunk) c = tiles / kLeastOfChunk;
   return (int)(c > kMostChunks ? kMostChunks : c < 2 ? 1 : c);
 }
@@ -459,7 +488,10 @@ size_t workspace_bytes_of(int64_t Hq, int64_t Hkv, int64_t Sq, int64_t Sk, int64
   const int c = chunks_of(Hq, Sq, Sk / 32);
   return panels_bytes(Hq, Hkv, Sq, Sk, D) + (c == 1 ? 0 : rows_bytes(Hq, Sq, c, 1) + rows_bytes(Hq, Sq, c, 2) + rows_bytes(Hq, Sq, c, D));
 }
-constexpr int64_t kMostOfPairs = 512;  // workgroups of a launch whose waves take two key tiles to a step
+// Workgroups of a launch whose waves take two key tiles to a step: where two of them to a compute unit, which is what the registers leave room for, are
+// all there are. us with one tile and with two: 32 / 8 heads x 2048, capped, 79.0 and 74.7, of heads of 64 60.9 and 56.1, 256 workgroups with a window of 4096
+// (not split) 121 and 114; 768 workgroups (64 / 8 x 1504) 39.9 and 45.8.
+constexpr int64_t kMostOfPairs = 512;
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
@@ -521,7 +553,8 @@ int amxfp4_attention_masked(const amx_format_t* fmt, int64_t q_heads, int64_t kv
   const int chunks = chunks_of(q_heads, Sq, (keys + 31) / 32);
   dim3 grid((unsigned)q_heads, (unsigned)((Sq + kQueries - 1) / kQueries));
   const int64_t workgroups = (int64_t)grid.x * grid.y;
-  if (workgroups > 256 && workgroups <= kMostOrdered && grid.y > 1 && grid.y <= 64) w.turn = q_heads < 256 ? (int)(256 / q_heads) : 1;
+  if (workgroups > 256 && grid.y > 1 && grid.y <= kMostBlocks)
+    w.turn = workgroups > kAtOnce ? (first || last ? (int)grid.y : 0) : q_heads < 256 ? (int)(256 / q_heads) : 1;
   const bool pairs = workgroups <= kMostOfPairs;
   if (chunks > 1) {
     uint8_t* at = static_cast<uint8_t*>(workspace) + panels_bytes(q_heads, kv_heads, Sq, Sk, head_dim);

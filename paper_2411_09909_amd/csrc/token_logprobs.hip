@@ -434,7 +434,7 @@ int parts_of(int dtype, int64_t rows, int64_t vocab, int& per_part) {
   // (a segment to each wave, or as many: with one more the others wait, and up to one each they need not be read again. 96 rows of 50001 BF16
   // logits in parts of four 13.7 us, of five 15.3)
   const int even = per_part / kWaves * kWaves;
-  if (even > 0 && (segments + even - 1) / even <= kMostParts) per_part = even;
+  if (parts > 1 && even > 0 && per_part < 4 * kWaves && (segments + even - 1) / even <= kMostParts) per_part = even;
   return (int)((segments + per_part - 1) / per_part);
 }
 
