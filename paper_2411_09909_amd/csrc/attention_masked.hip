@@ -468,24 +468,31 @@ __global__ __launch_bounds__(256) void attention_masked_join_kernel(const float*
 constexpr int64_t kAtOnce = 768;
 constexpr int64_t kMostBlocks = 64;  // (a lane to each)
 
-// Few workgroups with long rows are split over the keys, into about kSplitInto workgroups (twice as many where one wave of four has rows at
-// all), with kLeastOfChunk key tiles or more to each: 10 rows behind 3000 keys, 32 / 8 heads of 128, 92 -> 33 us (with four tiles 37), behind 30000 786 ->
-// 118 (132 with half as many), 100 rows of heads of 64 behind 8000 185 -> 46 (52 with twice as many), 700 rows behind 3000 116 -> 108 (111).
-constexpr int64_t kSplitBelow = 256, kSplitInto = 768, kLeastOfChunk = 8, kMostChunks = 64;
+// Few workgroups with long rows are split over the keys, kLeastOfChunk key tiles or more to a chunk, into as many as run at once: two to a
+// compute unit, or three with heads of 64, where the chunks stay long. us for up to 512, 768 and 1024 workgroups: 10 rows behind 30000 keys, 32 / 8 heads of
+// 128, 114, 131 and 117 (786 without a split), 200 rows of 40 heads behind 8000 90, 111 and 100, heads of 64, 100 rows behind 8000 42, 45 and 50 (185), 10 rows
+// behind 30000 81, 66 and 81. 10 rows behind 3000 keys in chunks of eight tiles 33, of four 37.
+constexpr int64_t kSplitBelow = 256, kLeastOfChunk = 8, kLongChunk = 32, kMostChunks = 64;
 
 // Chunks that the key tiles of a block of queries are cut into.
-int chunks_of(int64_t Hq, int64_t Sq, int64_t tiles) {
+int chunks_of(int64_t Hq, int64_t Sq, int64_t tiles, int64_t D) {
   const int64_t workgroups = Hq * ((Sq + kQueries - 1) / kQueries);
   if (workgroups > kSplitBelow) return 1;
-  int64_t c = ((Sq <= 32 ? 2 : 1) * kSplitInto + workgroups - 1) / workgroups;
+  int64_t c = 768 / workgroups;
+  if (D == 128 || tiles / c < kLongChunk) c = 512 / workgroups;
   if (c > tiles / kLeastOfChunk) c = tiles / kLeastOfChunk;
   return (int)(c > kMostChunks ? kMostChunks : c < 2 ? 1 : c);
+}
+// (the most for fewer tiles too)
+int most_chunks_of(int64_t Hq, int64_t Sq, int64_t tiles, int64_t D) {
+  const int a = chunks_of(Hq, Sq, tiles, D), b = chunks_of(Hq, Sq, tiles, 128);
+  return a > b ? a : b;
 }
 
 size_t panels_bytes(int64_t Hq, int64_t Hkv, int64_t Sq, int64_t Sk, int64_t D) { return (attention_workspace_bytes(Hq, Hkv, Sq, Sk, D) + 255) & ~(size_t)255; }
 size_t rows_bytes(int64_t Hq, int64_t Sq, int chunks, int64_t floats) { return ((size_t)(Hq * Sq * chunks * floats) * sizeof(float) + 255) & ~(size_t)255; }
 size_t workspace_bytes_of(int64_t Hq, int64_t Hkv, int64_t Sq, int64_t Sk, int64_t D) {
-  const int c = chunks_of(Hq, Sq, Sk / 32);
+  const int c = most_chunks_of(Hq, Sq, Sk / 32, D);
   return panels_bytes(Hq, Hkv, Sq, Sk, D) + (c == 1 ? 0 : rows_bytes(Hq, Sq, c, 1) + rows_bytes(Hq, Sq, c, 2) + rows_bytes(Hq, Sq, c, D));
 }
 // Workgroups of a launch whose waves take two key tiles to a step: where two of them to a compute unit, which is what the registers leave room for, are
@@ -550,7 +557,7 @@ int amxfp4_attention_masked(const amx_format_t* fmt, int64_t q_heads, int64_t kv
   uint16_t* out = static_cast<uint16_t*>(out_bf16);
   // (keys behind the last row's position are not seen: no more chunks than there is room for)
   const int64_t keys = causal && pos0 + Sq < Sk ? pos0 + Sq : Sk;
-  const int chunks = chunks_of(q_heads, Sq, (keys + 31) / 32);
+  const int chunks = chunks_of(q_heads, Sq, (keys + 31) / 32, head_dim);
   dim3 grid((unsigned)q_heads, (unsigned)((Sq + kQueries - 1) / kQueries));
   const int64_t workgroups = (int64_t)grid.x * grid.y;
   if (workgroups > 256 && grid.y > 1 && grid.y <= kMostBlocks)
