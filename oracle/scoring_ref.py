@@ -28,11 +28,12 @@ def cast_weights(p, scale_format, asymmetric):
     return ref.dequantize(c, s, TILE, scale_format, asymmetric)
 
 
-def cast_between(p, delta, scale_format, asymmetric):
+def cast_between(p, delta, scale_format, asymmetric, near=0.0):
     """How far apart the casts of weights within the relative error delta of p [32] may lie, element by element: the scale is that of the
-    group's largest (1 +- delta; exactly 1 where it holds the running maximum), an element is monotone in the weight where the scale is given."""
+    group's largest (1 +- delta; exactly 1 where it holds the running maximum), an element is monotone in the weight where the scale is given.
+    near: a largest weight that is so near below 1 counts as 1 (what ties in exact arithmetic need not in FP32)."""
     values = []
-    for top in (1.0,) if p.max() == 1 else (1 - delta, 1 + delta):
+    for top in (1.0,) if p.max() == 1 else (1 - delta, 1 + delta) + ((1 / p.max(),) if p.max() >= 1 - near else ()):
         for own in (1 - delta, 1.0, 1 + delta):
             q = p * own
             q[np.argmax(p)] = p.max() * top
@@ -48,7 +49,8 @@ def masked_attention(q_bits, k_bits, v_bits, scale, causal=True, pos0=0, first=N
     allowed, for a BF16 result out of FP32 arithmetic:
       - a score is a sum of D products, off by D 2^-24 B (B = scale sum |q k|); scaling, tanh (2^-22 of the cap) and distances add 2^-22 of
         (B + cap + slope distance) each; exp2 and its argument 2^-22: a weight is off by delta, relatively, twice that for a difference of scores;
-      - a weight next to a rounding boundary of the cast may fall on either side: cast_between();
+      - a weight next to a rounding boundary of the cast may fall on either side: cast_between(); a tile's largest score within 2^-16 + 2^-22
+        of its size (in log2) of the running maximum counts as it;
       - the sums: 2^-22 for each tile's steps, a factor's argument 2^-23 of the largest score (in log2) each time the maximum moves;
       - the BF16 result: half a step, 2^-8 of it."""
     Hq, Sq, D = q_bits.shape
@@ -87,7 +89,8 @@ def masked_attention(q_bits, k_bits, v_bits, scale, causal=True, pos0=0, first=N
                 p_hat = cast_weights(p[None], scale_format, asymmetric)[0]
                 v = vh[t0:t0 + TILE]
                 l, o = l * alpha + p.sum(), o * alpha + p_hat @ v
-                slack = slack * alpha + cast_between(p, delta, scale_format, asymmetric) @ np.abs(v)
+                near = 2.0 ** -16 + 2.0 ** -22 * 1.5 * (B + cap + far) + delta
+                slack = slack * alpha + cast_between(p, delta, scale_format, asymmetric, near) @ np.abs(v)
                 weight = weight * alpha + p_hat @ np.abs(v)
                 m, tiles = m_new, tiles + 1
             out[i, h] = o / l

@@ -53,8 +53,30 @@ def check(Hq, Hkv, Sq, Sk, D, kind=ref.FP8_E5M2, asym=1, causal=True, pos0=0, fi
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("kind,asym", FORMATS)
 @pytest.mark.parametrize("cap,sloped", [(0.0, False), (20.0, False), (0.0, True), (3.0, True)])
-def test_formats_and_scores(kind, asym, D, cap, sloped):
-    check(4, 2, 100, 128, D, kind, asym, cap=cap, slopes=slopes_of(4) if sloped else None)
+@pytest.mark.parametrize("Sk", [128, 288])  # K and V held whole; brought in by pairs of tiles
+def test_formats_and_scores(kind, asym, D, cap, sloped, Sk):
+    check(4, 2, 100, Sk, D, kind, asym, cap=cap, pos0=Sk - 110, slopes=slopes_of(4) if sloped else None)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kind,asym", FORMATS)
+@pytest.mark.parametrize("cap,sloped", [(0.0, False), (500.0, False), (0.0, True), (500.0, True)])
+@pytest.mark.parametrize("Sq,Sk", [(70, 288), (150, 320)])
+def test_many_workgroups_walk_tile_by_tile(Sq, Sk, cap, sloped, kind, asym, D):
+    """More workgroups than take two tiles to a step; some heads and rows of them against the oracle."""
+    H, fmt, at = 534, binding.make_format(kind, asym), [0, 267, 533]
+    gen = torch.Generator("cuda").manual_seed(Sq + D)
+    q, k, v = (torch.randn((n, s, D), generator=gen, device="cuda").to(torch.bfloat16) for n, s in ((H, Sq), (H // 2, Sk), (H // 2, Sk)))
+    ops = [*binding.quantize_batched(fmt, q), *binding.quantize_batched(fmt, k), *binding.quantize_batched(fmt, v, k_axis=1)]
+    slopes = torch.rand(H, generator=gen, device="cuda") if sloped else None
+    first = torch.randint(-5, Sk - Sq, (Sq,), generator=gen, device="cuda").int()
+    out = binding.attention_masked(fmt, *ops, D ** -0.5, pos0=Sk - Sq, first=first, cap=cap, slopes=slopes)
+    u16 = lambda x, n: x[n].cpu().view(torch.int16).numpy().view(np.uint16)  # noqa: E731
+    of = [h // 2 for h in at]
+    want, allowed = scoring_ref.masked_attention(u16(q, at), u16(k, of), u16(v, of), D ** -0.5, True, Sk - Sq, first.cpu().numpy(), None, cap,
+                                                 slopes[at].cpu().numpy() if sloped else None, kind, asym, rows := [0, 5, 31, 32, 63, Sq - 1])
+    got = out.view(Sq, H, D)[:, at].double().cpu().numpy()
+    assert torch.isfinite(out).all() and (np.abs(got - want) <= allowed)[rows].all()
 
 
 DOCUMENTS = [1, 2, 31, 32, 1, 33, 64, 5, 40, 7]  # 216 rows
