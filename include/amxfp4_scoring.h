@@ -60,7 +60,8 @@ typedef struct {
  *   workspace   at least amxfp4_attention_masked_workspace_bytes() bytes (which are more than amxfp4_attention's), 256-byte aligned
  *               (AMX_ERR_WORKSPACE otherwise).
  * The same call gives the same bits. (Few rows against many keys are split over the keys: each range's maxima first, so that every tile is
- * cast against the running maximum of all keys before it, as without the split.)
+ * cast against the running maximum of all keys before it, as without the split. Keys that a slope puts 2^-60 and more below a row's sum,
+ * by the norms of the queries and keys, may not be looked at.)
  */
 size_t amxfp4_attention_masked_workspace_bytes(const amx_format_t* fmt, int64_t q_heads, int64_t kv_heads, int64_t Sq, int64_t Sk,
                                                int64_t head_dim);

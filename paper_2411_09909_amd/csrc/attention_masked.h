@@ -18,9 +18,10 @@
 // independent; but the maximum is a fifth of the work (half of the products and no exponentials). One launch takes every chunk's
 // maxima, the next starts each chunk with those of the chunks before it, and the join adds the sums up: the same numbers as without the split.
 //
-// Bound and measured (us a call with the expansion of K and V in front; cards differ by 4 %): 32 / 8 heads of 128 x 8192 with slopes 580 = 948 TFLOP/s of
-// the visible half, with nothing but the causal mask 536 (amxfp4_attention: 567), the rate of a library's product of 8192^3 being 1200 to 1420. A
-// tile of a wave is 16 products of 32 cycles and some 600 cycles of vector instructions, 1200 together: the two pipes hardly overlap. 2048 rows of nine
+// Bound and measured (us a call with the expansion of K and V in front; cards differ by 4 %): 32 / 8 heads of 128 x 8192 with nothing but the causal mask 536 = 1026
+// TFLOP/s of the visible half (amxfp4_attention: 567), the rate of a library's product of 8192^3 being 1380 to 1420. A tile of a wave is 16 products of
+// 32 cycles and some 600 to 860 cycles of vector instructions (with slopes the maximum moves in every tile, and 64 registers of the output with it); counters: the
+// vector unit 83 % busy, the products 44 %, one beside the other. With slopes 590, and 367 to 390 without the tiles that are too far to count. 2048 rows of nine
 // documents with capped scores 42, of which the expansion is 8: blocks of very different length, all running at once. The first form took 834 and 55: the
 // accumulator in the second half of the register file, copied back and forth (waves_per_eu given no lower bound), the mask computed for every
 // tile, exp2 and a reciprocal for each capped score, two exchanges through LDS to a tile.
@@ -40,6 +41,7 @@ struct MaskedWork {
   int Sq, Sk, kv_group, causal, pos0;
   float *maxima, *parts;  // of split rows: [head][row][chunk]; [head][chunk][row][D]
   float2* ends;           // [head][chunk][row]: maximum and sum
+  const float* norms;     // [key head][key tile]: the largest norm of a key of the tile; nullptr: no tiles are left out
   int turn;  // query blocks to a turn of the workgroups over the compute units (0: the last block first)
   Scores scores;
 };
@@ -103,7 +105,13 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
   // x walks the query heads, a contiguous range of them per XCD where their number is a multiple of 8; y the query blocks: without ranges the
   // last ones, which have the most key tiles under a causal mask, first
   const int nheads = (int)gridDim.x;
-  const int h = (nheads & 7) == 0 ? (int)(blockIdx.x & 7) * (nheads >> 3) + (int)(blockIdx.x >> 3) : (int)blockIdx.x;
+  int h = (nheads & 7) == 0 ? (int)(blockIdx.x & 7) * (nheads >> 3) + (int)(blockIdx.x >> 3) : (int)blockIdx.x;
+  // (With far tiles left out heads of steep slopes have little to do: neighbours go to different XCDs, back and forth, and a compute unit's next
+  // workgroup, some 32 further on its XCD, is of another head than its last.)
+  if (SLOPE && w.norms && (nheads & 7) == 0) {
+    const int n = nheads >> 3, slot = (int)((blockIdx.x >> 3) + blockIdx.y * (uint32_t)n / 32) % n, xcd = (int)(blockIdx.x & 7);
+    h = 8 * slot + (slot & 1 ? 7 - xcd : xcd);
+  }
   const int g = h / w.kv_group;
   const int blocks = (int)gridDim.y;
   int block = blocks - 1 - (int)blockIdx.y;
@@ -212,7 +220,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
       }
       *reinterpret_cast<u32x4*>(all_tiles + (small_tiles * kFrags + i) * kFragBytes + lane_off) = values;
     }
-  } else {
+  } else if (!(SLOPE && PASS == kWhole)) {
     if (t_begin < t_end) load(t_begin, ldsK0, ldsV0);
   }
 
@@ -237,6 +245,46 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
     }
   }
 
+  // ---- far tiles. A key whose score is 60 below a row's maximum in units of log2 (2^-60 of the row's sum, for up to 2^20 of them) changes no bit of
+  // the result, and tiles in front of the first that may have others need not be looked at: their maximum is as far below, so that what is
+  // cast against it would not be seen either. |q . k| <= |q| |k| bounds the scores: a tile's by its largest key, the maximum's by the nearest
+  // key, from which the distances count.
+  const float slope = SLOPE ? w.scores.slopes[h] * kLog2e : 0.f;
+  const int nearest = none ? 0 : max(lo, min(position, lo + (int)span));
+  const int all_nearest = SLOPE ? wave_min(none ? 0x7FFFFFFF : nearest) : 0;
+  if constexpr (SLOPE && PASS == kWhole) {
+    if (w.norms && slope > 0.f) {  // uniform
+      float size = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < kFrags; ++kb)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) size = __builtin_fmaf((float)qf[kb][i], (float)qf[kb][i], size);
+      size += __shfl_xor(size, 32, 64);
+      const float* norms = w.norms + (int64_t)g * (w.Sk / 32);
+      size = __builtin_sqrtf(size) * w.scores.scale * 1.001f;  // (the cap makes scores smaller only)
+      float near = none ? 0.f : norms[nearest >> 5];
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) size = fmaxf(size, __shfl_xor(size, d, 64)), near = fmaxf(near, __shfl_xor(near, d, 64));
+      int skipped = own_begin;
+      for (; skipped < own_end; skipped += 64) {
+        const int t = skipped + lane;
+        const bool far = t < own_end && size * (norms[min(t, w.Sk / 32 - 1)] + near) + 60.f < slope * (float)(all_nearest - 32 * t - 31);
+        const uint64_t needed = ~__builtin_amdgcn_ballot_w64(far);
+        if (needed) {
+          skipped += (int)__builtin_ctzll(needed);
+          break;
+        }
+      }
+      own_begin = min(skipped, own_end);
+      __syncthreads();  // (the edges have been read)
+      if (lane == 0) edges[0][wave] = own_begin < own_end ? own_begin : 0x7FFFFFFF;
+      __syncthreads();
+      const int first = min(min(edges[0][0], edges[0][1]), min(edges[0][2], edges[0][3]));
+      t_begin = __builtin_amdgcn_readfirstlane(min(max(first, t_begin), t_end));
+    }
+    if (t_begin < t_end) load(t_begin, ldsK0, ldsV0);
+  }
+
   f32x16 o[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
@@ -251,9 +299,6 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
   // Distances are taken from the nearest key that the query sees: all its scores shift alike, and stay small where it sees far keys
   // only. In a tile in front of all the wave's nearest keys a score is f(q.k) + slope (key in the tile) - slope (distance of the tile's first
   // key): the second term is the last addition of f, the third is left to the maximum.
-  const float slope = SLOPE ? w.scores.slopes[h] * kLog2e : 0.f;
-  const int nearest = none ? 0 : max(lo, min(position, lo + (int)span));
-  const int all_nearest = SLOPE ? wave_min(none ? 0x7FFFFFFF : nearest) : 0;
   float step[16];
   if constexpr (SLOPE) {
 #pragma unroll
@@ -524,6 +569,37 @@ __global__ __launch_bounds__(256) void attention_masked_join_kernel(const float*
 
 }  // namespace
 
+// The largest norm of the keys of a tile, to a wave.
+template <int SCALE_KIND>
+__global__ __launch_bounds__(256) void key_norms_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int asym, int64_t tiles, int D,
+                                                        float* __restrict__ norms) {
+  const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (tile >= tiles) return;
+  const int lane = threadIdx.x & 63;
+  const int64_t key = tile * 32 + (lane & 31);  // (tiles of a head after another)
+  float sum = 0.f;
+  for (int i = lane >> 5; i < D / 32; i += 2) {
+    const u32x4 c = *reinterpret_cast<const u32x4*>(codes + key * (D / 2) + 16 * i);
+    const uint8_t* sb = scales + (key * (D / 32) + i) * (asym ? 2 : 1);
+    const float p = scale_value<SCALE_KIND>(sb[0]), n = asym ? scale_value<SCALE_KIND>(sb[1]) : p;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t word = c[j];
+      const f32x2 e[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.0f, 1),
+                          __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.0f, 3)};
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float v = e[k >> 1][k & 1], x = v * (v < 0.f ? n : p);
+        sum = __builtin_fmaf(x, x, sum);
+      }
+    }
+  }
+  sum += __shfl_xor(sum, 32, 64);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) sum = fmaxf(sum, __shfl_xor(sum, d, 64));
+  if (lane == 0) norms[tile] = __builtin_sqrtf(sum) * 1.001f;
+}
+
 // The launches of a checked call with heads of D. chunks > 1: split rows; small: kHeld; else pairs of key tiles to a step or not.
 template <int D>
 hipError_t launch_masked(int scale_kind, const MaskedOperands& m, const MaskedWork& w, int64_t q_heads, int chunks, bool small, bool pairs,
@@ -534,6 +610,11 @@ hipError_t launch_masked(int scale_kind, const MaskedOperands& m, const MaskedWo
       hipLaunchKernelGGL((attention_masked_kernel<SK, D, CAP, SLOPE, NT, PASS>), grid, dim3(64 * kWaves), 0, s, m.Q_codes, m.Q_scales, m.asym,
                          m.K_panel, m.V_panel, m.out, w, m.K_codes, m.K_scales, m.V_codes, m.V_scales);
     };
+    if (SLOPE && w.norms) {
+      const int64_t tiles = q_heads / w.kv_group * (w.Sk / 32);
+      hipLaunchKernelGGL((key_norms_kernel<SK>), dim3((unsigned)((tiles + 3) / 4)), dim3(256), 0, s, m.K_codes, m.K_scales, m.asym, tiles, D,
+                         const_cast<float*>(w.norms));
+    }
     if (chunks > 1) {
       pass.template operator()<2, kMaxima>();
       pass.template operator()<2, kPart>();

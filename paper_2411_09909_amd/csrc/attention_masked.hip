@@ -8,6 +8,9 @@ namespace {
 // unit that got a long block in one gets a short one in the next: nine documents in 2048 rows 47 -> 42 us, five prefixes in 1504 rows (64 heads)
 // 48 -> 40. Of more workgroups the longest start first.
 constexpr int64_t kAtOnce = 768;
+// Keys from which tiles too far for a slope are looked for, where no `first` cuts the rows shorter (the norms are a launch more). With and without, us: 32 / 8 heads
+// x 8192 with slopes from 2^-0.25 to 2^-8 367 and 590, of heads of 64 309 and 443, 40 / 8 heads x 4096 156 and 211, 32 / 8 x 2048 69 and 67.
+constexpr int64_t kFarKeys = 4096;
 constexpr int64_t kMostBlocks = 64;  // (a lane to each)
 
 // Few workgroups with long rows are split over the keys, kLeastOfChunk key tiles or more to a chunk, into as many as run at once: two to a
@@ -35,7 +38,7 @@ size_t panels_bytes(int64_t Hq, int64_t Hkv, int64_t Sq, int64_t Sk, int64_t D) 
 size_t rows_bytes(int64_t Hq, int64_t Sq, int chunks, int64_t floats) { return ((size_t)(Hq * Sq * chunks * floats) * sizeof(float) + 255) & ~(size_t)255; }
 size_t workspace_bytes_of(int64_t Hq, int64_t Hkv, int64_t Sq, int64_t Sk, int64_t D) {
   const int c = most_chunks_of(Hq, Sq, Sk / 32, D);
-  return panels_bytes(Hq, Hkv, Sq, Sk, D) + (c == 1 ? 0 : rows_bytes(Hq, Sq, c, 1) + rows_bytes(Hq, Sq, c, 2) + rows_bytes(Hq, Sq, c, D));
+  return panels_bytes(Hq, Hkv, Sq, Sk, D) + (size_t)(Hkv * (Sk / 32)) * sizeof(float) + (c == 1 ? 0 : rows_bytes(Hq, Sq, c, 1) + rows_bytes(Hq, Sq, c, 2) + rows_bytes(Hq, Sq, c, D));
 }
 // Workgroups of a launch whose waves take two key tiles to a step: where two of them to a compute unit, which is what the registers leave room for, are
 // all there are. us with one tile and with two: 32 / 8 heads x 2048, capped, 79.0 and 74.7, of heads of 64 60.9 and 56.1, 256 workgroups with a window of 4096
@@ -103,6 +106,8 @@ int amxfp4_attention_masked(const amx_format_t* fmt, int64_t q_heads, int64_t kv
     w.ends = reinterpret_cast<float2*>(at += rows_bytes(q_heads, Sq, chunks, 1));
     w.parts = reinterpret_cast<float*>(at += rows_bytes(q_heads, Sq, chunks, 2));
   }
+  if (w.scores.slopes && !first && chunks == 1 && Sk >= kFarKeys)
+    w.norms = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + panels_bytes(q_heads, kv_heads, Sq, Sk, head_dim));
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const bool asym = fmt->asymmetric != 0;
   uint16_t* Kp = static_cast<uint16_t*>(workspace);

@@ -79,6 +79,32 @@ def test_many_workgroups_walk_tile_by_tile(Sq, Sk, cap, sloped, kind, asym, D):
     assert torch.isfinite(out).all() and (np.abs(got - want) <= allowed)[rows].all()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kind,asym", [(ref.FP8_E5M2, 1), (ref.E8M0_FLOOR, 0)])
+@pytest.mark.parametrize("H,cap,ranged", [(180, 0.0, False), (184, 0.0, True), (304, 20.0, False)])
+def test_far_tiles_that_slopes_leave_out(H, cap, ranged, kind, asym, D):
+    """Slopes from steep ones, of which the near keys alone count, to none and negative ones; far keys that are large enough to count all the same."""
+    Sq, Sk, fmt = 150, 4128, binding.make_format(kind, asym)
+    gen = torch.Generator("cuda").manual_seed(H + D)
+    q, k, v = (torch.randn((n, s, D), generator=gen, device="cuda").to(torch.bfloat16) for n, s in ((H, Sq), (H // 2, Sk), (H // 2, Sk)))
+    k[:, ::97] *= 8
+    k[:, 333] *= 60
+    ops = [*binding.quantize_batched(fmt, q), *binding.quantize_batched(fmt, k), *binding.quantize_batched(fmt, v, k_axis=1)]
+    slopes = torch.exp2(torch.rand(H, generator=gen, device="cuda") * 12 - 9)
+    at = [0, 1, 2, 3, H // 2, H - 1]
+    slopes[at] = torch.tensor([0.5, 0.1, 0.03, 4.0, 0.0, -0.01], device="cuda")
+    last = torch.randint(Sk - Sq - 2000, Sk, (Sq,), generator=gen, device="cuda").int() if ranged else None
+    if ranged:
+        last[40:80] = -1
+    out = binding.attention_masked(fmt, *ops, D ** -0.5, pos0=Sk - Sq, last=last, cap=cap, slopes=slopes)
+    u16 = lambda x, n: x[n].cpu().view(torch.int16).numpy().view(np.uint16)  # noqa: E731
+    of, n = [h // 2 for h in at], lambda x: None if x is None else x.cpu().numpy()  # noqa: E731
+    want, allowed = scoring_ref.masked_attention(u16(q, at), u16(k, of), u16(v, of), D ** -0.5, True, Sk - Sq, None, n(last), cap, n(slopes[at]),
+                                                 kind, asym, rows := [0, 31, 77, 128, Sq - 1])
+    got = out.view(Sq, H, D)[:, at].double().cpu().numpy()
+    assert torch.isfinite(out).all() and (np.abs(got - want) <= allowed)[rows].all()
+
+
 DOCUMENTS = [1, 2, 31, 32, 1, 33, 64, 5, 40, 7]  # 216 rows
 
 
