@@ -13,11 +13,10 @@
 // Alternatives. A row is read in segments (chunks of 16 bytes to a lane, side by side over the wave); each leaves its largest logit
 // in LDS, each thread keeps its own. The top-th largest of a wave's 64 and of the segments' bound the result from below, so only
 // segments that reach the bound are read again, from the cache, and the few elements at or above it are put in order by counting for
-// each how many are better. Rows in which more than kList elements reach the bound (equal logits by the hundred, fewer tokens than `top`
-// not ruled out) take them one after the other.
+// each how many are better. Rows in which more than kList elements reach the bound (equal logits by the hundred) take them one after the other.
 //
 // Bound and measured: 4096 rows of 128000 float32 logits, 10 alternatives, 381 us = 5.5 TB/s (reads alone reach 6.2), 700 of 256000, capped, 139 us = 5.1 TB/s, where the
-// vector unit is 67 % busy; one row of 128000 11 us, two launches of a chain each: read, bound, list, order. The first form took 391, 156 and 22 us: it ranked the
+// vector unit is 67 % busy; one row of 128000 11.5 us, two launches of a chain each: read, bound, list, order. The first form took 391, 156 and 22 us: it ranked the
 // threads' maxima through LDS, read every segment again, took one place in the list at a time and both functions of a cap for every logit.
 #include "kernels.h"
 #include "scoring.h"
@@ -120,11 +119,12 @@ struct Selection {
 
 // The k best of the elements that each(f) hands to this thread as f(logit, id, there), k in all threads together, in order: emit(rank, logit,
 // id). f comes for N elements at a time, `there` false for those that are none. No element below `bound` is among them. What is not there (of
-// rows with NaN) comes out as id -1. l.count is 0.
+// rows with NaN) comes out as id -1. l.count is 0. Where the bound is -inf and the list too short, it is made again of what is not ruled out and of
+// those others that `early` says yes to, the lowest ids: no more of them can be wanted.
 template <int N, class Each, class Emit>
 __device__ __forceinline__ void select_best(Selection& l, int k, float bound, Each each, Emit emit) {
   const int t = threadIdx.x;
-  each([&](const float (&v)[N], auto id, auto there) {
+  each([&](const float (&v)[N], auto id, auto there, auto) {
     int mine = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) mine += v[i] >= bound && there(i) ? 1 : 0;
@@ -138,7 +138,22 @@ __device__ __forceinline__ void select_best(Selection& l, int k, float bound, Ea
       }
   });
   __syncthreads();
-  const int n = l.count;
+  int n = l.count;
+  if (n > kList && bound == -INFINITY) {  // (uniform) parts of a row that are ruled out: 20 rows of 60000, half of them so, 42 us without, 16 with it
+    __syncthreads();
+    if (t == 0) l.count = 0;
+    __syncthreads();
+    each([&](const float (&v)[N], auto id, auto there, auto early) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (there(i) && (v[i] > -INFINITY || (v[i] == -INFINITY && early(i)))) {
+          const int at = atomicAdd(&l.count, 1);
+          if (at < kList) l.list[at] = key_of(v[i], id(i));
+        }
+    });
+    __syncthreads();
+    n = l.count;
+  }
   if (n <= kList) {
     for (int c = t; c < n; c += kThreads) {
       const uint64_t key = l.list[c];
@@ -153,7 +168,7 @@ __device__ __forceinline__ void select_best(Selection& l, int k, float bound, Ea
   uint64_t last = ~uint64_t(0);
   for (int r = 0; r < k; ++r) {
     uint64_t best = 0;  // (less than any element's)
-    each([&](const float (&v)[N], auto id, auto there) {
+    each([&](const float (&v)[N], auto id, auto there, auto) {
 #pragma unroll
       for (int i = 0; i < N; ++i)
         if (v[i] >= bound && there(i)) {
@@ -346,7 +361,8 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(LogprobWork w)
       auto segment = [&](int s) {
         const int first = s * kSegment - off + lane * kE;
         auto id = [&](int i) { return first + i / kE * 64 * kE + i % kE; };
-        f(v, id, [&](int i) { return id(i) >= 0 && id(i) < w.vocab; });
+        // (fewer than k of a part's first 2 k ids are not ruled out where any that is may be wanted)
+        f(v, id, [&](int i) { return id(i) >= 0 && id(i) < w.vocab; }, [&](int i) { return id(i) < max(s0 * kSegment - off, 0) + 2 * k; });
       };
       if (segments <= kWaves) {  // a wave has read one at most, and has it still
         if (wave < segments) segment(s0 + wave);
@@ -409,7 +425,8 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_join_kernel(LogprobWo
       for (int i = t; i < parts * k; i += kThreads) {
         const uint2 entry = tops[i];
         const float v[1] = {u2f(entry.x)};
-        f(v, [&](int) { return (int)entry.y; }, [&](int) { return (int)entry.y >= 0; });
+        // (the first part, of more than k ids, names as many as can be wanted)
+        f(v, [&](int) { return (int)entry.y; }, [&](int) { return (int)entry.y >= 0; }, [&](int) { return i < k; });
       }
     };
     auto emit = [&](int rank, float v, int id) {

@@ -116,6 +116,23 @@ def test_tokens_ruled_out(vocab, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [70, 2999, 33000, 128000])
+def test_tokens_whole_parts_ruled_out(vocab, dtype):
+    rng = np.random.RandomState(vocab + 1)
+    x = logits_of(rng, 6, vocab, dtype)
+    x[0, vocab // 3:] = -INF
+    x[1, :vocab // 2] = -INF
+    x[2] = -INF
+    x[3, 40:] = -INF
+    x[4, :-30] = -INF
+    x[5, rng.rand(vocab) < 0.999] = -INF
+    for top in (20, 64):
+        check(x, [0, vocab - 1, 5, 39, vocab - 1, 0], top)
+        for row in range(6):            # (one row alone is in parts)
+            check(x[row:row + 1], [1], top, 5.0 * (row % 2))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("vocab", [30, 2000, 60000])
 def test_what_is_not_a_number(vocab, dtype):
     rng = np.random.RandomState(vocab)
