@@ -37,7 +37,8 @@ inline Scores scores_of(const amx_scores_t* s, float scale) {
     // as far as the powers of c stay in range: with a wide cap fewer terms up to a smaller size, with a very narrow one none
     if (c < 0x1p12f && scale < 0x1p20f) {
       const int terms = c > 0x1p-12f ? 3 : c > 0x1p-30f ? 2 : 1;
-      r.small = (terms == 3 ? kSmall : terms == 2 ? 0.02f : 0x1p-12f) / c;
+      // (2^60: the polynomial squares the product)
+      r.small = fminf((terms == 3 ? kSmall : terms == 2 ? 0.02f : 0x1p-12f) / c, 0x1p60f);
       r.k1 = r.scale * u * kTanh[0];
       if (terms >= 2) r.k2 = r.scale * u * u * kTanh[1];
       if (terms == 3) r.k3 = r.scale * u * u * u * kTanh[2];
