@@ -496,8 +496,17 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
       }
       if constexpr (SCORED) {
         if (w.scores.cap > 0.f) {
+          // (exp2 and a reciprocal alone are off by 2^-22 of the cap: with caps of 2^16 and more, in the weights' first percent)
+          float size = __builtin_fabsf(y[0]);
 #pragma unroll
-          for (int k = 0; k < kMine; ++k) y[k] = capped(y[k], w.scores.in, w.scores.cap);
+          for (int k = 1; k < kMine; ++k) size = fmaxf(size, __builtin_fabsf(y[k]));
+          if (__builtin_amdgcn_ballot_w64(size > w.scores.small) == 0) {  // uniform
+#pragma unroll
+            for (int k = 0; k < kMine; ++k) y[k] = capped_small(y[k], w.scores, 0.f);
+          } else {
+#pragma unroll
+            for (int k = 0; k < kMine; ++k) y[k] = capped_any(y[k], w.scores);
+          }
         } else {
 #pragma unroll
           for (int k = 0; k < kMine; ++k) y[k] *= w.scores.scale;

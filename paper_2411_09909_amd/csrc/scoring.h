@@ -61,4 +61,9 @@ __device__ __forceinline__ float capped_small(float s, const Scores& w, float pl
   return __builtin_fmaf(s, p, plus);
 }
 
+// Of any product, each by what is its due.
+__device__ __forceinline__ float capped_any(float s, const Scores& w) {
+  return __builtin_fabsf(s) <= w.small ? capped_small(s, w, 0.f) : capped(s, w.in, w.cap);
+}
+
 }  // namespace amx
