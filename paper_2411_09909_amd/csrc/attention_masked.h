@@ -65,6 +65,9 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {  // (what is n
 // 12 heads of 64 x 77 10.0 -> 8.3 us, 32 / 8 heads of 128 x 20 and x 128 9.6 -> 8.0; 64 heads of 64 x 250 13.6 either way.
 constexpr int kHeldElements = 16384;
 constexpr float kLowest = -0x1.fffffep127f;
+// Added to a sum of up to 128 squares that is to bound a norm from above: squares below 2^-126, those of numbers below 2^-63, are too small or lost
+// (a scale of 2^80 makes large scores of such numbers).
+constexpr float kLostSquares = 0x1p-118f;
 constexpr int kWaves = 4, kQueries = 32 * kWaves;  // waves and queries of a workgroup
 
 __device__ __forceinline__ int wave_min(int v) {
@@ -261,7 +264,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
         for (int i = 0; i < 8; ++i) size = __builtin_fmaf((float)qf[kb][i], (float)qf[kb][i], size);
       size += __shfl_xor(size, 32, 64);
       const float* norms = w.norms + (int64_t)g * (w.Sk / 32);
-      size = __builtin_sqrtf(size) * w.scores.scale * 1.001f;  // (the cap makes scores smaller only)
+      size = __builtin_sqrtf(size + kLostSquares) * w.scores.scale * 1.001f;  // (the cap makes scores smaller only)
       float near = none ? 0.f : norms[nearest >> 5];
 #pragma unroll
       for (int d = 16; d > 0; d >>= 1) size = fmaxf(size, __shfl_xor(size, d, 64)), near = fmaxf(near, __shfl_xor(near, d, 64));
@@ -597,7 +600,7 @@ __global__ __launch_bounds__(256) void key_norms_kernel(const uint8_t* __restric
   sum += __shfl_xor(sum, 32, 64);
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) sum = fmaxf(sum, __shfl_xor(sum, d, 64));
-  if (lane == 0) norms[tile] = __builtin_sqrtf(sum) * 1.001f;
+  if (lane == 0) norms[tile] = __builtin_sqrtf(sum + kLostSquares) * 1.001f;
 }
 
 // The launches of a checked call with heads of D. chunks > 1: split rows; small: kHeld; else pairs of key tiles to a step or not.
