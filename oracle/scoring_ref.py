@@ -129,13 +129,30 @@ def paged_attention(q, pool, table, lens, starts, positions, softmax_scale, scal
     return out, weight, size
 
 
+def allowed_logprobs(p, z, vocab, cap):
+    """(of a log probability, of an entropy), as token_logprobs() counts them; z: distances from the largest value, p: their probabilities."""
+    segments = -(-min(-(-(vocab + 7) // 1024), 512) // 4)  # of a wave
+    s = 16 * segments * 2.0 ** -24 + segments * 7 * 2.0 ** -24 + 30 * 5 * 2.0 ** -24 + 2.0 ** -21
+    with np.errstate(over="ignore", invalid="ignore"):
+        counts = p > 0
+        A, Q = (p[counts] * -z[counts]).sum(), (p[counts] * z[counts] ** 2).sum()
+    value = 1.25 * 2.0 ** -21 * cap
+    of_s = s + value + A * 2.0 ** -22  # relative, of the sum
+    # of the sum of exponentials times distances, over the sum
+    of_t = value + A * (s + value + 2.0 ** -22) + Q * 2.0 ** -22
+    return of_s + value, of_s + of_t + A * of_s
+
+
 def token_logprobs(logits, targets, top, cap):
     """float64 logits [rows, vocab]. Returns (logprob, entropy, top_logprobs, top_ids, allowed of a log probability, allowed of an entropy).
 
-    allowed: a logit in units of log2 is off by 2^-23 of itself, a capped one by 2^-22 of the cap at most; a thread adds up to vocab / 64
-    terms one after another, each off by 2^-22 (its exponential) and rounded once, and a hundred joins are rounded: S by
-    (vocab / 64 + 128) 2^-24 + 2^-21, relatively, and T the same in units of the largest distance that counts (weights below e^-40 do not);
-    the results are rounded, twice at most."""
+    allowed, in the order of a thread's work, with z = x - m the distance from the largest value, A = sum p |z| and Q = sum p z^2:
+      - a value is off by 2^-22 of the cap (a quarter more where tanh is near -1), a distance by two of those and 2^-24 of itself, an exponential by that,
+        the rounding of its argument and 2^-22; a thread's maximum moves on from 0 to m in steps, whose factors' arguments add up to |z| again;
+      - a thread reads every fourth of at most 512 segments of 1024 values, 16 of each, one after another: a rounding of 2^-24 to each, for the sum of
+        exponentials and that of exponentials times distances, which both have terms of one sign; and with each segment a factor (2^-22) and up to
+        three roundings;
+      - some 30 joins (64 lanes, 4 waves, 64 parts) of 2^-22 and 2^-24 each; the logarithm and what is added behind it 2^-21."""
     rows, vocab = logits.shape
     live = logits > -np.inf
     with np.errstate(invalid="ignore", over="ignore"):
@@ -153,13 +170,12 @@ def token_logprobs(logits, targets, top, cap):
             logprob[r] = -np.inf if inside else 0.0
             continue
         m = y[seen].max()
-        lse = m + np.log(np.exp(y[seen] - m).sum())
-        z = y - lse
+        z = y - m
+        lse = np.log(np.exp(z[seen]).sum())
+        distance, z = z, z - lse
         logprob[r] = z[targets[r]] if inside else 0.0
-        entropy[r] = -(np.exp(z[seen]) * z[seen]).sum()
+        p = np.exp(z[seen])
+        entropy[r] = -(p * z[seen]).sum()
         tops[r] = z[ids[r]]
-        size = np.abs(y[seen][y[seen] >= m - 40]).max() + cap
-        s = (vocab / 64 + 128) * 2.0 ** -24 + 2.0 ** -21
-        off[r] = 2 * 2.0 ** -22 * size + s + 2.0 ** -22
-        off_entropy[r] = (2 * 2.0 ** -22 * size + s) * (2 + 2 * entropy[r] + 40)
+        off[r], off_entropy[r] = allowed_logprobs(p, distance[seen], vocab, cap)
     return logprob, entropy, tops, ids, off, off_entropy
