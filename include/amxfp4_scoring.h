@@ -90,7 +90,9 @@ int amxfp4_paged_attention_scored(const amx_format_t* fmt, const amx_paged_pool_
  *     entropy      = -sum_v p_v (x_v - lse)   (of tokens with p_v > 0), in nats
  *     top_ids, top_logprobs   the `top` largest logits in descending order, of equal ones the lowest id first; x - lse of each
  * A row of which all logits are -inf: logprob (of a target inside) and top_logprobs -inf, entropy 0, ids 0, 1, ... A row with a logit of NaN or
- * +inf (or of a magnitude above 2^127): logprob (of a target inside), entropy and top_logprobs may be NaN, ids any (within the vocabulary, or -1).
+ * +inf: logprob (of a target inside), entropy and top_logprobs may be NaN, ids any (within the vocabulary, or -1).
+ * Finite logits may be of any size, the type's lowest value (as which a token may be ruled out: with a cap it is -cap, as any other) among them; a log
+ * probability below FP32's range is -inf.
  *   logits     dtype 0 = float32, 1 = BF16; [rows][ld], ld >= vocab, aligned to its elements' size. Columns from vocab on are not looked at. A product's
  *              output (amxfp4_gemm: C, ldc) as it is.
  *   targets    int32 [rows], or NULL; logprob [rows], NULL exactly when targets is; entropy [rows], or NULL.

@@ -8,7 +8,8 @@
 // (Differences first and log2 e after them: the largest logit's is exactly 0, whatever its size.)
 //
 // A capped logit is x (1 + u P(u)), u = (x / cap)^2, up to 0.6 of the cap, which is most segments; in the others each value takes what
-// is its due. Logits of -inf have a path of their own too: there the differences are kept from 0 times infinity.
+// is its due. Logits of -inf, or so far below the largest that FP32 does not hold the difference, have a path of their own too: there the
+// differences are kept from 0 times infinity.
 //
 // Alternatives. A row is read in segments (chunks of 16 bytes to a lane, side by side over the wave); each leaves its largest logit
 // in LDS, each thread keeps its own. The top-th largest of a wave's 64 and of the segments' bound the result from below, so only
@@ -301,7 +302,7 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(LogprobWork w)
     const float m = fmaxf(mine.m, value_of<CAP>(w, most)), to = m == -INFINITY ? 0.f : m;
     mine = shifted(mine, to);
     mine.m = m;
-    if (__builtin_amdgcn_ballot_w64(CAP ? edge > w.small : edge == -INFINITY) == 0) {  // uniform
+    if (__builtin_amdgcn_ballot_w64(CAP ? edge > w.small : edge - to == -INFINITY) == 0) {  // uniform
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
         const float z = (CAP ? capped_small(w, v[i]) : v[i]) - to, e = __builtin_amdgcn_exp2f(z * kLog2e);
@@ -311,7 +312,7 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(LogprobWork w)
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
         const float z = value_of<CAP>(w, v[i]) - to, e = __builtin_amdgcn_exp2f(z * kLog2e);
-        mine.s += e, mine.t = __builtin_fmaf(e, fmaxf(z, -1000.f), mine.t);  // (0 times -inf)
+        mine.s += e, mine.t = __builtin_fmaf(e, fmaxf(z, -1000.f), mine.t);  // (0 times -inf, which a difference of large ones may be too)
       }
     }
   }
