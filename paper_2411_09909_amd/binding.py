@@ -223,6 +223,14 @@ def make_format(scale=FP8_E5M2, asymmetric=True, group_size=32):
     return AmxFormat(int(group_size), 0, int(scale), int(bool(asymmetric)))
 
 
+def _cap(cap):
+    """The cap of a call as a float. (Its limits are checked here: as float32, as which the library gets it, a tiny one would be 0, which is none.)"""
+    cap = float(cap)
+    if cap != 0 and not 2.0 ** -20 <= cap <= 2.0 ** 20:
+        raise AmxError("cap must be 0 or 2^-20 to 2^20, not %g" % cap)
+    return cap
+
+
 def _groups(fmt, K):
     """Groups along a row of K elements (group_size -1: the whole row is one group)."""
     return 1 if fmt.group_size == -1 else K // fmt.group_size
@@ -837,8 +845,9 @@ def paged_attention(fmt, q, pool, table, lens, starts, positions, scale, max_key
     and positions out of paged_plan()). max_keys: at least the longest sequence, 0 if not known. Returns BF16 [rows, q_heads *
     head_dim]; rows behind the last sequence's are left as they were (zeros in a new tensor). cap, slopes: amxfp4_paged_attention_scored, as for
     attention_masked()."""
+    cap = _cap(cap)
     if out is not None and workspace is not None:
-        more = (float(cap), slopes) if cap or slopes is not None else ()
+        more = (cap, slopes) if cap or slopes is not None else ()
         rc = (_calls or _bound()).paged_attention(fmt, q, pool, table, lens, starts, positions, float(scale), max_keys, out, workspace, *more)
         if rc is not None:
             return out if rc == 0 else _check(rc)
@@ -875,7 +884,7 @@ def _scores(cap, slopes, q_heads):
             raise AmxError("slopes must be float32 [%d], not %s of %s" % (q_heads, slopes.dtype, tuple(slopes.shape)))
     elif not cap:
         return None
-    return ctypes.byref(AmxScores(float(cap), 0, None if slopes is None else slopes.data_ptr()))
+    return ctypes.byref(AmxScores(cap, 0, None if slopes is None else slopes.data_ptr()))
 
 
 def attention_masked_workspace_bytes(fmt, q_heads, kv_heads, Sq, Sk, head_dim=128):
@@ -888,9 +897,10 @@ def attention_masked(fmt, q_codes, q_scales, k_codes, k_scales, v_codes, v_scale
     last[i] (int32 [Sq], or None: all) and, with `causal`, none behind its position. cap > 0: scores s become cap tanh(s / cap); slopes float32
     [q_heads]: they fall by slopes[h] for each key of distance. Operands as for attention() (contiguous). Returns BF16 [Sq, q_heads * head_dim];
     rows that see nothing are zeros."""
+    cap = _cap(cap)
     operands = (q_codes, q_scales, k_codes, k_scales, v_codes, v_scales)
     if out is not None and workspace is not None:
-        rc = (_calls or _bound()).attention_masked(fmt, *operands, float(scale), bool(causal), pos0, first, last, float(cap), slopes, out, workspace)
+        rc = (_calls or _bound()).attention_masked(fmt, *operands, float(scale), bool(causal), pos0, first, last, cap, slopes, out, workspace)
         if rc is not None:
             return out if rc == 0 else _check(rc)
     _here(*operands)
@@ -939,9 +949,10 @@ def token_logprobs(logits, targets=None, top=0, cap=0.0, out=None, workspace=Non
     """amxfp4_token_logprobs: float32 or BF16 logits [rows, vocab] (rows any distance apart) -> TokenLogprobs: the log probability of each
     row's target (int32 [rows]; 0 for one outside the vocabulary), the row's entropy, and the log probabilities and ids of its `top` largest
     logits. cap > 0: logits x become cap tanh(x / cap) first. out: the buffers of a TokenLogprobs, float32 and int32."""
+    cap = _cap(cap)
     if out is not None and workspace is not None:
         out = out if type(out) is TokenLogprobs else TokenLogprobs(*out)
-        rc = (_calls or _bound()).token_logprobs(logits, targets, top, float(cap), out, workspace)
+        rc = (_calls or _bound()).token_logprobs(logits, targets, top, cap, out, workspace)
         if rc is not None:
             return out if rc == 0 else _check(rc)
     _need_cuda(logits)
@@ -966,6 +977,6 @@ def token_logprobs(logits, targets=None, top=0, cap=0.0, out=None, workspace=Non
     _here(logits[:0], workspace)
     at = [None if t is None or t.numel() == 0 else t.data_ptr() for t in (targets,) + out]
     _check(load().amxfp4_token_logprobs(logits.data_ptr(), 1 if logits.dtype == torch.bfloat16 else 0, rows, vocab,
-                                        logits.stride(0) if rows > 1 else vocab, at[0], float(cap), int(top), at[1], at[2], at[3], at[4],
+                                        logits.stride(0) if rows > 1 else vocab, at[0], cap, int(top), at[1], at[2], at[3], at[4],
                                         workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
     return out
