@@ -268,6 +268,8 @@ class LMHead:
     def logprobs(self, x, targets=None, top=0):
         """binding.token_logprobs() of the rows x BF16 [rows, d_model]."""
         rows = x.shape[0]
+        if targets is not None:  # (all of them: a part's would not show one too many)
+            binding._ints(rows, targets)
         f = lambda *shape: torch.empty(shape, dtype=torch.float32, device=x.device)  # noqa: E731
         out = binding.TokenLogprobs(None if targets is None else f(rows), f(rows), f(rows, top) if top else None,
                                     torch.empty((rows, top), dtype=torch.int32, device=x.device) if top else None)
