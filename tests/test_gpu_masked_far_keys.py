@@ -1,5 +1,5 @@
-"""Far keys under a slope, which the masked attention may leave out by the norms of queries and keys: keys whose squares FP32 does not hold.
-Against 64 bits, as test_gpu_attention_masked."""
+"""Far keys under a slope, which the masked attention may leave out by the norms of queries and keys: keys whose squares FP32 does not hold, what
+leaving keys out may cost. Against 64 bits, as test_gpu_attention_masked."""
 import numpy as np
 import pytest
 import torch
@@ -39,3 +39,22 @@ def test_keys_whose_squares_vanish(small, scale, kind, asym, D):
     slopes = torch.full((H,), 1.5 * D / 128, device="cuda")
     got, want, allowed = run(H, q, k, v, 2.0 ** scale, slopes, kind, asym, at, rows)
     assert (np.abs(want) > 0.1).any() and (np.abs(got - want) <= allowed).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kind,asym", [(ref.E8M0_FLOOR, 0), (ref.E8M0_ROUND, 1), (ref.FP8_E5M2, 1)])
+def test_large_values_of_far_keys(kind, asym, D):
+    """Keys that a slope puts far below a row's sum may be left out, each by up to 2^-60 of its value: where near values are zero, or far ones larger by more
+    than that, a result is so far off and no further."""
+    H, at, rows = 184, [0, 1, 91, 183], [0, 31, 64, SQ - 1]
+    gen = torch.Generator("cuda").manual_seed(D + 1)
+    q, k, v = (torch.randn((n, s, D), generator=gen, device="cuda").to(torch.bfloat16) for n, s in ((H, SQ), (1, SK), (1, SK)))
+    size = 2.0 ** 100 if kind != ref.FP8_E5M2 else 2.0 ** 14
+    v[0, :1000] *= size
+    v[0, 1000:, :D // 2] = 0
+    slopes = torch.full((H,), 0.5, device="cuda")
+    slopes[at] = torch.tensor([0.05, 0.02, 4.0, 0.0], device="cuda")
+    got, want, allowed = run(H, q, k, v, D ** -0.5, slopes, kind, asym, at, rows)
+    # (a weight left out is below 2^-60 of the sum, and a cast one below 2^-59: the scale of the cast is a tile's largest weight's; values are below 8 times `size`)
+    assert (np.abs(got - want) <= allowed + SK * 2.0 ** -59 * 8 * size).all()
+    assert (np.abs(got - want) <= allowed)[:, 3].all()  # no slope: nothing is left out
