@@ -36,7 +36,7 @@ extern "C" {
 typedef struct {
   float cap;           /* 0: none; else 2^-20 to 2^20 */
   int32_t reserved;    /* 0 */
-  const float* slopes; /* device, [q_heads], finite, 4-byte aligned, or NULL */
+  const float* slopes; /* device, [q_heads], finite (beyond 2^90 either way as 2^90), 4-byte aligned, or NULL */
 } amx_scores_t;
 
 /*
@@ -63,7 +63,7 @@ typedef struct {
  *               (AMX_ERR_WORKSPACE otherwise).
  * The same call gives the same bits. (Few rows against many keys are split over the keys: each range's maxima first, so that every tile is
  * cast against the running maximum of all keys before it, as without the split. Keys that a slope puts 2^-60 and more below a row's sum,
- * by the norms of the queries and keys, may not be looked at.)
+ * by the norms of the queries and keys, may not be looked at: each leaves the result off by up to 2^-59 of its value.)
  */
 size_t amxfp4_attention_masked_workspace_bytes(const amx_format_t* fmt, int64_t q_heads, int64_t kv_heads, int64_t Sq, int64_t Sk,
                                                int64_t head_dim);

@@ -248,11 +248,12 @@ __global__ __launch_bounds__(64 * kWaves, NT == 2 ? 2 : D == 64 ? 4 : 3) void at
     }
   }
 
-  // ---- far tiles. A key whose score is 60 below a row's maximum in units of log2 (2^-60 of the row's sum, for up to 2^20 of them) changes no bit of
-  // the result, and tiles in front of the first that may have others need not be looked at: their maximum is as far below, so that what is
-  // cast against it would not be seen either. |q . k| <= |q| |k| bounds the scores: a tile's by its largest key, the maximum's by the nearest
+  // ---- far tiles. A key whose score is 60 below a row's maximum in units of log2 has less than 2^-60 of the row's sum, and is left out where a bound
+  // on its score says so: the result is off by that much of the key's value. (Values as large as to show it, 2^50 times the near ones, are the caller's
+  // to keep out.) Tiles in front of the first that may have others need not be looked at: their maximum is as far below, so that what is
+  // cast against it would be as small. |q . k| <= |q| |k| bounds the scores: a tile's by its largest key, the maximum's by the nearest
   // key, from which the distances count.
-  const float slope = SLOPE ? w.scores.slopes[h] * kLog2e : 0.f;
+  const float slope = SLOPE ? slope_of(w.scores, (uint32_t)h) : 0.f;
   const int nearest = none ? 0 : max(lo, min(position, lo + (int)span));
   const int all_nearest = SLOPE ? wave_min(none ? 0x7FFFFFFF : nearest) : 0;
   if constexpr (SLOPE && PASS == kWhole) {

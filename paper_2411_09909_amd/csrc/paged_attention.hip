@@ -406,7 +406,7 @@ __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 :
     float m = -INFINITY, l = 0.f;
     const float sc = SCORED ? 1.0f : w.scale_log2;
     float slope = 0.f;
-    if (SCORED && w.scores.slopes) slope = asked ? w.scores.slopes[(uint32_t)head * (uint32_t)w.per + head_of] * kLog2e : 0.f;
+    if (SCORED && w.scores.slopes) slope = asked ? slope_of(w.scores, (uint32_t)head * (uint32_t)w.per + head_of) : 0.f;
 
     for (; tile < stop; tile += SHARE) {
       const bool more = tile + SHARE < stop;

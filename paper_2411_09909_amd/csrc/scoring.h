@@ -47,6 +47,11 @@ inline Scores scores_of(const amx_scores_t* s, float scale) {
   return r;
 }
 
+// The slope of a query head. Distances are below 2^31, and what a slope makes of them has to be finite: the nearest key has all the weight well before.
+__device__ __forceinline__ float slope_of(const Scores& w, uint32_t head) {
+  return fminf(fmaxf(w.slopes[head] * kLog2e, -0x1p90f), 0x1p90f);
+}
+
 // cap * tanh from what the product is: the two hardware functions are right to about an ulp of 1, so the result to 2^-22 of the
 // cap, absolutely. An infinite exponential gives the cap itself.
 __device__ __forceinline__ float capped(float s, float in, float cap) {
