@@ -439,8 +439,9 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_join_kernel(LogprobWo
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-// Parts that a row is read in, and segments of each: as many as give 1024 workgroups, and more for long rows, up to 3000, as long as a part has
-// 128 KB. Rows of 1024 and more are read whole. us with up to 1024, 2048 and 4096 workgroups: 300 rows of 32000 BF16 logits 16.5, 21.5 and
+// Parts that a row is read in, and segments of each: as many as give 1024 workgroups, and more for long rows, up to 3000 workgroups, as long as a part has
+// 128 KB (so up to 1500 rows of 256 KB and more are read in two parts at least, from 1501 on whole); whatever the number of rows, as many as keep a part's
+// segments within kSegments. us with up to 1024, 2048 and 4096 workgroups: 300 rows of 32000 BF16 logits 16.5, 21.5 and
 // 19.1, 2000 of 128000 BF16 120, 132 and 146, 700 of 256000 float32 154, 140 and 135, 4000 of 32001 float32 108, 108 and 122.
 int parts_of(int dtype, int64_t rows, int64_t vocab, int& per_part) {
   const int64_t segments = (vocab + 7 + kSegment - 1) / kSegment;  // (a row may begin up to 7 elements behind a boundary)
@@ -454,7 +455,7 @@ int parts_of(int dtype, int64_t rows, int64_t vocab, int& per_part) {
   parts = parts > least ? parts : least;
   per_part = (int)((segments + parts - 1) / parts);
   // (a segment to each wave, or as many: with one more the others wait, and up to one each they need not be read again. 96 rows of 50001 BF16
-  // logits in parts of four 13.7 us, of five 15.3)
+  // logits in parts of four 13.7 us, of five 15.3; 14.3 since ruled-out parts are listed once more)
   const int even = per_part / kWaves * kWaves;
   if (parts > 1 && even > 0 && per_part < 4 * kWaves && (segments + even - 1) / even <= kMostParts) per_part = even;
   return (int)((segments + per_part - 1) / per_part);
