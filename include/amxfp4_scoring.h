@@ -30,7 +30,7 @@ extern "C" {
  *     cap > 0:         s = cap * tanh(s / cap)
  *     slopes != NULL:  s = s - slopes[h] * |p - j|        (h: the query head)
  * in this order. Both in FP32. The tanh is right to about 2^-22 of cap, absolutely (1 - 2 / (1 + exp 2x)). Scores up to 0.45 of the cap (from a cap of
- * 4096 scale on up to 0.02 of it, from 2^30 scale on 2^-12) are right to 2^-20 of themselves (a polynomial): over the paged cache each by itself, in a prompt
+ * 4096 scale on, and of scales up to 2^-20, up to 0.02 of it, from 2^30 scale on 2^-12) are right to 2^-21 of themselves (a polynomial): over the paged cache each by itself, in a prompt
  * where those of 32 neighbouring rows and 32 or 64 neighbouring keys all are so small. Raw products above 2^60 count as large.
  */
 typedef struct {
