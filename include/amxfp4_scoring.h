@@ -46,6 +46,8 @@ typedef struct {
  *     and, with causal != 0, j <= p only,
  * the same for all heads. Over these the recurrence of amxfp4_attention: key tiles of 32 in ascending order, the probabilities of a
  * tile cast as one group of `fmt` against the running maximum. A row that sees no key gives zeros.
+ * (Weights come out of FP32 scores, so one next to a boundary of the cast may be cast to either side; a tile whose largest score, in units of log2, is within
+ * 2^-16 and 2^-22 of itself of the running maximum counts as holding it in a power-of-two scale.)
  *   documents   packed into one pass: first[i] = where row i's document begins, causal.
  *   prefixes    read in both directions: last[i] = the end of the prefix for its rows, p for those behind it; causal = 0.
  *   windows     first[i] = p - window + 1, causal.

@@ -21,8 +21,8 @@
 // Bound and measured (us a call with the expansion of K and V in front; cards differ by 4 %): 32 / 8 heads of 128 x 8192 with nothing but the causal mask 536 = 1026
 // TFLOP/s of the visible half (amxfp4_attention: 567), the rate of a library's product of 8192^3 being 1380 to 1420. A tile of a wave is 16 products of
 // 32 cycles and some 600 to 860 cycles of vector instructions (with slopes the maximum moves in every tile, and 64 registers of the output with it); counters: the
-// vector unit 83 % busy, the products 44 %, one beside the other. With slopes 590, and 367 to 390 without the tiles that are too far to count. 2048 rows of nine
-// documents with capped scores 42, of which the expansion is 8: blocks of very different length, all running at once. The first form took 834 and 55: the
+// vector unit 83 % busy, the products 44 %, one beside the other. With slopes 590, and 364 to 392 without the tiles that are too far to count. 2048 rows of nine
+// documents with capped scores 39 to 42, of which the expansion is 8: blocks of very different length, all running at once (the longest alone takes 37). The first form took 834 and 55: the
 // accumulator in the second half of the register file, copied back and forth (waves_per_eu given no lower bound), the mask computed for every
 // tile, exp2 and a reciprocal for each capped score, two exchanges through LDS to a tile.
 #pragma once

@@ -197,8 +197,8 @@ struct PagedTile {
 };
 
 // SHARE: waves to a sequence and key head, 4 or 1. SCORED: scores are capped, or fall with distance, or both (include/amxfp4_scoring.h); they
-// are in units of log2 from there on. (32 / 8 heads of 128, capped, with slopes and neither: one sequence of 700 tokens 10.9, 11.0 and 10.3 us, 48 of up to 12000
-// 79.6, 79.3 and 77.9; 150 of up to 900 and three rows, heads of 64, 26.5, 26.0 and 24.5.)
+// are in units of log2 from there on. (32 / 8 heads of 128, capped, with slopes and neither: one sequence of 700 tokens 10.9, 10.9 and 10.4 us, 48 of up to 12000
+// 79.1, 79.4 and 77.9; 150 of up to 900 and three rows, heads of 64, 26.8, 26.2 and 24.4.)
 template <int SCALE_KIND, bool ASYM, int D, int GC, int SHARE, bool SCORED>
 __global__ __launch_bounds__(256, D == 64 || GC == 4 || (!ASYM && GC == 2) ? 3 : 2) void paged_attention_kernel(
     PagedPool pool, PagedWork w, const int32_t* __restrict__ table, const int32_t* __restrict__ lens, const int32_t* __restrict__ starts,

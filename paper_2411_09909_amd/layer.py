@@ -83,7 +83,7 @@ class DecoderLayer:
     def __init__(self, cfg, weights, fmt, baseline=False, fused_attention=False, fused_glu=None, fused_norm=None,
                  fused_rope=None, prepared_weights=False, slopes=None):
         """slopes: float32 [n_heads] on the GPU: scores of a head fall by so much for each key of distance (with or without a cap, these need
-        fused_attention in forward())."""
+        fused_attention in forward()). They come beside the rotary embedding, which is always there."""
         self.cfg, self.fmt, self.baseline, self.fused_attention = cfg, fmt, baseline, fused_attention
         self.slopes = slopes
         # the rotary embedding casts its result (Q and K never exist as BF16 tensors): same bits
@@ -141,7 +141,7 @@ class DecoderLayer:
     def forward(self, x, pos0=0, first=None, last=None):
         """x BF16 [rows, d_model], rows a multiple of 32, the first at position pos0. first, last: int32 [rows] on the GPU: the first and the last of
         these rows that each of them sees, as binding.attention_masked() takes them (last instead of the causal mask: none behind the row
-        itself is kept from it then); they need fused_attention."""
+        itself is kept from it then); they need fused_attention. step() knows no such ranges: its rows see all that their sequence holds up to them."""
         c = self.cfg
         masked = first is not None or last is not None or c.score_cap or self.slopes is not None
         if masked and not self.fused_attention:
@@ -254,7 +254,8 @@ class DecoderLayer:
 
 class LMHead:
     """What turns the last layer's output into log probabilities of tokens. weight: BF16 CUDA tensor [vocab, d_model], cast once here; norm: FP32
-    [d_model], the normalisation in front of it; cap: logits x become cap tanh(x / cap). The logits exist for `rows_at_once` rows at a time."""
+    [d_model], the normalisation in front of it; cap: logits x become cap tanh(x / cap). The logits exist for `rows_at_once` rows at a time. (Where
+    the format multiplies in BF16 the weights are expanded for each such part: 4096 rows of 4096 against 128000 tokens 4.7 ms in parts of 1024, 3.7 at once.)"""
 
     def __init__(self, weight, norm, fmt, eps=1e-5, cap=0.0, rows_at_once=1024):
         self.fmt, self.eps, self.cap, self.rows_at_once = fmt, eps, cap, rows_at_once
