@@ -224,8 +224,8 @@ def make_format(scale=FP8_E5M2, asymmetric=True, group_size=32):
 
 
 def _cap(cap):
-    """The cap of a call as a float. (Its limits are checked here: as float32, as which the library gets it, a tiny one would be 0, which is none.)"""
-    cap = float(cap)
+    """The cap of a call as a float, 0 for None. (Its limits are checked here: as float32, as which the library gets it, a tiny one would be 0, which is none.)"""
+    cap = 0.0 if cap is None else float(cap)
     if cap != 0 and not 2.0 ** -20 <= cap <= 2.0 ** 20:
         raise AmxError("cap must be 0 or 2^-20 to 2^20, not %g" % cap)
     return cap

@@ -31,3 +31,7 @@ def test_caps_that_float32_does_not_hold_are_refused(monkeypatch, cap):
             with pytest.raises(binding.AmxError, match="cap"):
                 call()
     assert not [n for n in reached if "workspace" not in n]
+
+
+def test_caps_in_range_and_none():
+    assert [binding._cap(c) for c in (None, 0, 0.0, -0.0, 30, 2.0 ** -20, 2 ** 20, torch.tensor(5.0))] == [0, 0, 0, 0, 30, 2.0 ** -20, 2.0 ** 20, 5]
